@@ -71,7 +71,12 @@ typedef enum {
   AOH_ERR_WORKSPACE = 4    /* decode workspace missing or too small */
 } aoh_status;
 
-typedef enum { AOH_BF16 = 0, AOH_F32 = 1 } aoh_dtype;
+typedef enum {
+  AOH_BF16 = 0,
+  AOH_F32 = 1,
+  AOH_E4M3 = 2, /* formats of the 8-bit caches only */
+  AOH_I8 = 3
+} aoh_dtype;
 
 /* Tokens per page of the paged cache and per block of the ring cache. */
 #define AOH_PAGE_TOKENS 16
@@ -298,6 +303,129 @@ aoh_status aoh_decode_step_noalloc(const aoh_tensor* q, const aoh_tensor* k_new,
                                    const aoh_paged_cache* kv_full, const aoh_ring_cache* kv_ring,
                                    const uint8_t* head_is_streaming, const int32_t* lens, int32_t n_sink,
                                    int32_t window, aoh_tensor* out, void* stream);
+
+/*
+ * ------------------------------------------------------------ 8-bit caches
+ * The two caches with K and V in 8 bits: half the resident bytes, and half of
+ * what a decode step reads.  Every row (one token, one KV head, K or V) has one
+ * power-of-two scale.  With amax = max_d |x_d| of the row,
+ *   E      = the least integer >= -100 with amax <= c 2^E
+ *            (c = 448 for AOH_E4M3, 127 for AOH_I8),
+ *   code_d = x_d 2^-E rounded to the nearest code, ties to even,
+ *   value_d = code_d 2^E,   scale byte = E + 127.
+ * x_d 2^-E is exact, so the stored bits depend on the row alone.  A value is off
+ * by at most 2^(E-1) < amax / 127 (AOH_I8), or by 2^-4 |x_d| and for
+ * |x_d| < 2^(E-6) by 2^(E-10) (AOH_E4M3).  A row that holds a NaN, an infinity or
+ * a magnitude of 2^127 or more is kept as NaN: scale byte 255, codes 0.
+ * AOH_E4M3 is the OCP fp8 format of that name (no infinities), AOH_I8 two's
+ * complement.  Both caches of a call have one format.
+ */
+
+/*
+ * Paged cache in 8 bits; pages, block table and errors as for aoh_paged_cache.
+ * A (page, head) is 16 rows:
+ *   k:      [num_pages][n_heads][16][D]            codes
+ *   v:      [num_pages][n_heads][D/4][4][4][4]     codes, element (row r,
+ *           dimension d) at [d / 4][r / 4][d % 4][r % 4]
+ *   scales: [num_pages][n_heads][16][2]            scale bytes of K and V
+ */
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* scales;
+  const int32_t* block_table;
+  int64_t num_pages;
+  int32_t max_pages_per_seq;
+  int32_t n_heads;
+  int32_t n_seqs; /* rows of block_table */
+  int32_t format; /* AOH_E4M3 or AOH_I8 */
+} aoh_paged_cache_q8;
+
+/*
+ * Ring cache in 8 bits; slots as for aoh_ring_cache, blocks of 16 slots laid out
+ * as the pages above:
+ *   k: [B][n_heads][Cpad/16][16][D]   v: [B][n_heads][Cpad/16][D/4][4][4][4]
+ *   scales: [B][n_heads][Cpad/16][16][2]
+ */
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* scales;
+  int32_t n_heads;
+  int32_t capacity;
+  int32_t batch;
+  int32_t format;
+} aoh_ring_cache_q8;
+
+/*
+ * aoh_kv_append into 8-bit caches: the same tokens to the same slots, quantised
+ * (bf16 or fp32 in).  start_pos may be NULL (every sequence starts at 0).
+ * Positions beyond the block table, in unmapped pages (entries outside
+ * [0, num_pages)) and of sequences with start_pos < 0 or >= 2^30 are not written.
+ */
+aoh_status aoh_kv_append_q8(const aoh_tensor* k_new, const aoh_tensor* v_new, const uint8_t* head_is_streaming,
+                            const int32_t* start_pos, const aoh_paged_cache_q8* kv_full,
+                            const aoh_ring_cache_q8* kv_ring, int32_t n_sink, int32_t window, void* stream);
+
+/*
+ * The same for token counts that differ, packed as in aoh_prefill_varlen:
+ * sequence b appends rows cu_seqlens[b] .. cu_seqlens[b+1]-1 of
+ *   k_new, v_new: [total][Hkv][D]
+ * at positions start_pos[b] on.  cu_seqlens: DEVICE int32 [batch + 1],
+ * non-decreasing (entries are clamped into [0, total]); max_new: HOST bound on
+ * every count (tokens past it are not written).
+ */
+aoh_status aoh_kv_append_q8_varlen(const aoh_tensor* k_new, const aoh_tensor* v_new, const int32_t* cu_seqlens,
+                                   int32_t batch, int32_t max_new, const uint8_t* head_is_streaming,
+                                   const int32_t* start_pos, const aoh_paged_cache_q8* kv_full,
+                                   const aoh_ring_cache_q8* kv_ring, int32_t n_sink, int32_t window, void* stream);
+
+/*
+ * Reads positions start_pos[b] + t, t < n, of every sequence back as the values
+ * they stand for (exact in bf16 and in fp32):
+ *   k_out, v_out: [B][n][Hkv][D], bf16 or fp32, written.
+ * A row is written where the cache of its head holds the position: start_pos[b]
+ * + t < lens[b], in a mapped page, and for a streaming head among the n_sink
+ * first or the `window` last of the lens[b] tokens.  All other rows are left as
+ * they were.  start_pos (may be NULL: 0), lens: DEVICE int32 [B]; a sequence
+ * with start_pos < 0 or >= 2^30 is left out.
+ */
+aoh_status aoh_kv_read_q8(const aoh_paged_cache_q8* kv_full, const aoh_ring_cache_q8* kv_ring,
+                          const uint8_t* head_is_streaming, const int32_t* start_pos, const int32_t* lens,
+                          int32_t n_sink, int32_t window, aoh_tensor* k_out, aoh_tensor* v_out, void* stream);
+
+/*
+ * Device workspace (bytes) of aoh_decode_q8 and aoh_decode_step_q8 for any step
+ * of `batch` sequences, Hq query heads of width d_head.  Returns 0 for invalid
+ * arguments.
+ */
+size_t aoh_decode_q8_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t d_head);
+
+/*
+ * aoh_decode over 8-bit caches: softmax(q . K / sqrt(D)) V over the values that
+ * the codes stand for, with q bf16 and sums in fp32.  Scales and codes enter
+ * exactly; each weight is rounded to bf16 before the product with V for a bf16
+ * out, and kept to 2^-17 of itself for an fp32 out.  A sequence with lens[b] <= 0
+ * (an empty place of a padded batch) gets 0.  Lengths are clamped to the block
+ * table's capacity.  AOH_ERR_UNSUPPORTED for fp32 q, for Hq / Hkv > 16 and for
+ * Hkv * (capacity of a sequence in 16-token blocks + 16) >= 2^29.
+ * Graph capture and workspace as for aoh_decode.
+ */
+aoh_status aoh_decode_q8(const aoh_tensor* q, const aoh_paged_cache_q8* kv_full, const aoh_ring_cache_q8* kv_ring,
+                         const uint8_t* head_is_streaming, const int32_t* lens, int32_t n_sink, int32_t window,
+                         aoh_tensor* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * aoh_decode_step over 8-bit caches: out and caches equal those of
+ * aoh_kv_append_q8 of the token at lens[b] - 1 followed by aoh_decode_q8, bit for
+ * bit, with one launch fewer.  k_new, v_new: [B][Hkv][D] bf16.  The page of
+ * position lens[b] - 1 must not be referenced by another block-table entry that
+ * the call reads.
+ */
+aoh_status aoh_decode_step_q8(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
+                              const aoh_paged_cache_q8* kv_full, const aoh_ring_cache_q8* kv_ring,
+                              const uint8_t* head_is_streaming, const int32_t* lens, int32_t n_sink, int32_t window,
+                              aoh_tensor* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * ---------------------------------------------------------------- H2Share

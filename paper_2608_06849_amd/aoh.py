@@ -18,10 +18,11 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libaoh.so")
 
 AOH_OK, AOH_ERR_INVALID_ARG, AOH_ERR_UNSUPPORTED, AOH_ERR_HIP, AOH_ERR_WORKSPACE = range(5)
-AOH_BF16, AOH_F32 = 0, 1
+AOH_BF16, AOH_F32, AOH_E4M3, AOH_I8 = range(4)
 PAGE_TOKENS = 16
 
 _DTYPES = {torch.bfloat16: AOH_BF16, torch.float32: AOH_F32}
+_FORMATS = {torch.float8_e4m3fn: AOH_E4M3, torch.int8: AOH_I8}  # of the 8-bit caches
 
 
 class AohError(RuntimeError):
@@ -46,10 +47,25 @@ class AohRingCache(ctypes.Structure):
                 ("capacity", ctypes.c_int32), ("batch", ctypes.c_int32)]
 
 
+class AohPagedCacheQ8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
+                ("max_pages_per_seq", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
+
+
+class AohRingCacheQ8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("n_heads", ctypes.c_int32), ("capacity", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
+
+
 _lib = None
 
 EXPORTS = ("aoh_prefill", "aoh_prefill_chunked", "aoh_prefill_append", "aoh_prefill_varlen", "aoh_kv_append", "aoh_decode_workspace_bytes", "aoh_decode", "aoh_decode_step",
            "aoh_decode_step_noalloc",
+           "aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8_workspace_bytes",
+           "aoh_decode_q8", "aoh_decode_step_q8",
            "aoh_classify_workspace_bytes", "aoh_classify", "aoh_retrieval_group_count",
            "aoh_head_mapping_workspace_bytes", "aoh_head_mapping", "aoh_decode_anchor_workspace_bytes",
            "aoh_decode_anchor", "aoh_decode_reuse_workspace_bytes", "aoh_decode_reuse",
@@ -98,6 +114,26 @@ def lib():
                                               P(AohRingCache), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
                                               ctypes.c_int32, P(AohTensor), ctypes.c_void_p]
         L.aoh_decode_step_noalloc.restype = ctypes.c_int
+        L.aoh_kv_append_q8.argtypes = [P(AohTensor), P(AohTensor), ctypes.c_void_p, ctypes.c_void_p,
+                                       P(AohPagedCacheQ8), P(AohRingCacheQ8), ctypes.c_int32, ctypes.c_int32,
+                                       ctypes.c_void_p]
+        L.aoh_kv_append_q8.restype = ctypes.c_int
+        L.aoh_kv_append_q8_varlen.argtypes = [P(AohTensor), P(AohTensor), ctypes.c_void_p, ctypes.c_int32,
+                                              ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, P(AohPagedCacheQ8),
+                                              P(AohRingCacheQ8), ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p]
+        L.aoh_kv_append_q8_varlen.restype = ctypes.c_int
+        L.aoh_kv_read_q8.argtypes = [P(AohPagedCacheQ8), P(AohRingCacheQ8), ctypes.c_void_p, ctypes.c_void_p,
+                                     ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, P(AohTensor), P(AohTensor),
+                                     ctypes.c_void_p]
+        L.aoh_kv_read_q8.restype = ctypes.c_int
+        L.aoh_decode_q8_workspace_bytes.argtypes = [ctypes.c_int32] * 3
+        L.aoh_decode_q8_workspace_bytes.restype = ctypes.c_size_t
+        L.aoh_decode_q8.argtypes = [P(AohTensor), P(AohPagedCacheQ8), P(AohRingCacheQ8), ctypes.c_void_p,
+                                    ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, P(AohTensor), ctypes.c_void_p,
+                                    ctypes.c_size_t, ctypes.c_void_p]
+        L.aoh_decode_q8.restype = ctypes.c_int
+        L.aoh_decode_step_q8.argtypes = [P(AohTensor)] * 3 + L.aoh_decode_q8.argtypes[1:]
+        L.aoh_decode_step_q8.restype = ctypes.c_int
         L.aoh_classify_workspace_bytes.argtypes = [ctypes.c_int32] * 4
         L.aoh_classify_workspace_bytes.restype = ctypes.c_size_t
         L.aoh_classify.argtypes = [P(AohTensor), P(AohTensor), ctypes.c_int32, ctypes.c_int32,
@@ -235,6 +271,76 @@ class RingCache:
         return c
 
 
+class PagedCacheQ8:
+    """Retrieval-head cache in 8 bits (torch.float8_e4m3fn or torch.int8): K codes [pages, heads, 16, D], V codes
+    [pages, heads, D/4, 4, 4, 4] (dim // 4, row // 4, dim % 4, row % 4), scale bytes [pages, heads, 16, 2] (K, V;
+    uint8), and a per-sequence block table (int32), all contiguous and on one device.  The object keeps the
+    descriptor that the calls pass on, so its tensors stay the same."""
+
+    def __init__(self, k, v, scales, block_table):
+        pages, heads, _, d = k.shape
+        _check_q8(k, v, scales, (pages, heads), d)
+        _check_i32(block_table, "block_table", k.device)
+        if block_table.dim() != 2:
+            raise ValueError("block_table must be [sequences, pages]")
+        self.k, self.v, self.scales, self.block_table = k, v, scales, block_table
+        self._desc = AohPagedCacheQ8(k.data_ptr(), v.data_ptr(), scales.data_ptr(), block_table.data_ptr(), pages,
+                                     block_table.shape[1], heads, block_table.shape[0], _FORMATS[k.dtype])
+        self._ref, self.device, self.width = ctypes.byref(self._desc), k.device, d
+
+    @classmethod
+    def allocate(cls, num_pages, n_heads, d, dtype, block_table, device="cuda"):
+        block_table = block_table.to(device=device, dtype=torch.int32).contiguous()
+        return cls(*_alloc_q8((num_pages, n_heads), d, dtype, device), block_table)
+
+    def rows(self, b0, b1):
+        """The same pages with block-table rows b0 .. b1-1 (sequences b0 .. b1-1)."""
+        return PagedCacheQ8(self.k, self.v, self.scales, self.block_table[b0:b1])
+
+
+class RingCacheQ8:
+    """Streaming-head cache in 8 bits: n_sink + window slots per (sequence, head), padded to whole 16-slot blocks,
+    each laid out as a page of PagedCacheQ8: K codes [batch, heads, blocks, 16, D] and so on."""
+
+    def __init__(self, k, v, scales, capacity):
+        batch, heads, blocks, _, d = k.shape
+        if blocks != (capacity + PAGE_TOKENS - 1) // PAGE_TOKENS:
+            raise ValueError(f"{blocks} blocks of {PAGE_TOKENS} slots for a capacity of {capacity}")
+        _check_q8(k, v, scales, (batch, heads, blocks), d)
+        self.k, self.v, self.scales, self.capacity = k, v, scales, capacity
+        self._desc = AohRingCacheQ8(k.data_ptr(), v.data_ptr(), scales.data_ptr(), heads, capacity, batch,
+                                    _FORMATS[k.dtype])
+        self._ref, self.device, self.width = ctypes.byref(self._desc), k.device, d
+
+    @classmethod
+    def allocate(cls, batch, n_heads, n_sink, window, d, dtype, device="cuda"):
+        cap = n_sink + window
+        nblk = (cap + PAGE_TOKENS - 1) // PAGE_TOKENS
+        return cls(*_alloc_q8((batch, n_heads, nblk), d, dtype, device), cap)
+
+
+def _alloc_q8(lead, d, dtype, device):
+    return (torch.empty((*lead, PAGE_TOKENS, d), dtype=dtype, device=device),
+            torch.empty((*lead, d // 4, 4, 4, 4), dtype=dtype, device=device),
+            torch.empty((*lead, PAGE_TOKENS, 2), dtype=torch.uint8, device=device))
+
+
+def _check_q8(k, v, scales, lead, d):
+    """The tensors of an 8-bit cache with units of `lead` dimensions."""
+    if k.dtype not in _FORMATS or v.dtype != k.dtype or scales.dtype != torch.uint8:
+        raise TypeError(f"codes must be float8_e4m3fn or int8 and scales uint8, not {k.dtype}, {v.dtype}, {scales.dtype}")
+    for t, name, shape in ((k, "k", (PAGE_TOKENS, d)), (v, "v", (d // 4, 4, 4, 4)), (scales, "scales", (PAGE_TOKENS, 2))):
+        if tuple(t.shape) != (*lead, *shape):
+            raise ValueError(f"{name} must be {(*lead, *shape)}, not {tuple(t.shape)}")
+        if not t.is_contiguous() or t.device != k.device:
+            raise ValueError(f"{name} must be contiguous and on one device with the others")
+
+
+def _check_i32(t, name, device):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor on {device}")
+
+
 # ----------------------------------------------------------------------------- entry points
 
 def aoh_prefill(q, k, v, head_is_streaming, n_sink, window, out=None, stream=None):
@@ -359,6 +465,137 @@ def aoh_decode_step_noalloc(q, k_new, v_new, kv_full, kv_ring, head_is_streaming
                                          _ptr(lens), n_sink, window, ctypes.byref(od), _stream(stream)))
     return out
 
+
+# ----------------------------------------------------------------------------- 8-bit caches
+
+def _q8_desc(t, name, device, width):
+    """aoh_tensor descriptor of a tensor that has to be on `device`, with rows of `width`."""
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the caches on {device}")
+    shape = t.shape
+    if len(shape) > 4 or not shape or shape[-1] != width:
+        raise ValueError(f"{name}: shape {tuple(shape)}, for caches of width {width}")
+    return AohTensor(t.data_ptr(), _DTYPES[t.dtype], len(shape), tuple(shape), t.stride())
+
+
+def _q8_caches(kv_full, kv_ring):
+    """Device and width of the caches, and their descriptors."""
+    if kv_full is None:
+        if kv_ring is None:
+            raise ValueError("no cache given")
+        one = kv_ring
+    else:
+        one = kv_full
+        if kv_ring is not None and (kv_ring.device != one.device or kv_ring.width != one.width):
+            raise ValueError("the caches differ in device or width")
+    if one.device.type != "cuda":
+        raise ValueError(f"the caches are on {one.device}")
+    return one.device, one.width, kv_full and kv_full._ref, kv_ring and kv_ring._ref
+
+
+def _q8_seqs(t, name, device, n):
+    """Pointer of a per-sequence int32 tensor of at least n entries."""
+    _check_i32(t, name, device)
+    if t.numel() < n:
+        raise ValueError(f"{name} has {t.numel()} entries for {n} sequences")
+    return t.data_ptr()
+
+
+def _q8_labels(head_is_streaming, n):
+    """Head labels as bytes, one for each of the n KV heads."""
+    m = bytes(map(int, head_is_streaming))
+    if len(m) != n:
+        raise ValueError(f"{len(m)} head labels for {n} KV heads")
+    return m
+
+
+def _q8_run(call, device, stream, *args):
+    """Calls with the device's current stream (or the given one) and that device current."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the caches on {device}")
+    if torch.cuda.current_device() == device.index:
+        _check(call(*args, stream.cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, stream.cuda_stream))
+
+
+def aoh_kv_append_q8(k_new, v_new, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, stream=None):
+    """Quantise k_new/v_new [B,n_new,Hkv,D] into 8-bit caches at positions start_pos[b] + t (None: t)."""
+    dev, d, full, ring = _q8_caches(kv_full, kv_ring)
+    kd, vd = _q8_desc(k_new, "k_new", dev, d), _q8_desc(v_new, "v_new", dev, d)
+    start = _q8_seqs(start_pos, "start_pos", dev, k_new.shape[0]) if start_pos is not None else None
+    m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
+    _q8_run(lib().aoh_kv_append_q8, dev, stream, kd, vd, m, start, full, ring, n_sink, window)
+
+
+def aoh_kv_append_q8_varlen(k_new, v_new, cu_seqlens, max_new, head_is_streaming, start_pos, kv_full, kv_ring, n_sink,
+                            window, stream=None):
+    """Quantise packed tokens k_new/v_new [total,Hkv,D] into 8-bit caches: sequence b's are rows cu_seqlens[b] ..
+    cu_seqlens[b+1]-1, at positions start_pos[b] on (None: 0 on)."""
+    dev, d, full, ring = _q8_caches(kv_full, kv_ring)
+    kd, vd = _q8_desc(k_new, "k_new", dev, d), _q8_desc(v_new, "v_new", dev, d)
+    n = cu_seqlens.numel() - 1
+    cu = _q8_seqs(cu_seqlens, "cu_seqlens", dev, 2) if n > 0 else None
+    start = _q8_seqs(start_pos, "start_pos", dev, n) if start_pos is not None else None
+    m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
+    _q8_run(lib().aoh_kv_append_q8_varlen, dev, stream, kd, vd, cu, n, max_new, m, start, full, ring, n_sink, window)
+
+
+def aoh_kv_read_q8(kv_full, kv_ring, head_is_streaming, start_pos, lens, n_sink, window, k_out, v_out, stream=None):
+    """Read positions start_pos[b] + t < lens[b] back into k_out/v_out [B,n,Hkv,D]; rows that the caches do not hold
+    are left as they were."""
+    dev, d, full, ring = _q8_caches(kv_full, kv_ring)
+    kd, vd = _q8_desc(k_out, "k_out", dev, d), _q8_desc(v_out, "v_out", dev, d)
+    b = k_out.shape[0]
+    start = _q8_seqs(start_pos, "start_pos", dev, b) if start_pos is not None else None
+    n = _q8_seqs(lens, "lens", dev, b)
+    m = _q8_labels(head_is_streaming, k_out.shape[-2] if k_out.dim() > 1 else 0)
+    _q8_run(lib().aoh_kv_read_q8, dev, stream, full, ring, m, start, n, n_sink, window, kd, vd)
+    return k_out, v_out
+
+
+def aoh_decode_q8_workspace_bytes(batch, n_q_heads, d_head):
+    return int(lib().aoh_decode_q8_workspace_bytes(batch, n_q_heads, d_head))
+
+
+def _decode_q8(call, new, q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out, workspace, stream):
+    dev, d, full, ring = _q8_caches(kv_full, kv_ring)
+    if out is None:
+        out = torch.empty_like(q)
+    qd, od = _q8_desc(q, "q", dev, d), _q8_desc(out, "out", dev, d)
+    kv = [_q8_desc(t, name, dev, d) for t, name in zip(new, ("k_new", "v_new"))]
+    n = _q8_seqs(lens, "lens", dev, q.shape[0])
+    m = _q8_labels(head_is_streaming, (kv_full.k.shape[1] if full else 0) + (kv_ring.k.shape[1] if ring else 0))
+    if workspace is None:
+        workspace = torch.empty(aoh_decode_q8_workspace_bytes(q.shape[0], q.shape[-2], d), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {dev}")
+    _q8_run(call, dev, stream, qd, *kv, full, ring, m, n, n_sink, window, od, workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())
+    return out
+
+
+def aoh_decode_q8(q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out=None, workspace=None, stream=None):
+    """One decode step over 8-bit caches: out[B,Hq,D] (bf16, or fp32 if `out` is) for queries at positions lens[b]-1;
+    0 where lens[b] is 0."""
+    return _decode_q8(lib().aoh_decode_q8, (), q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out,
+                      workspace, stream)
+
+
+def aoh_decode_step_q8(q, k_new, v_new, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out=None,
+                       workspace=None, stream=None):
+    """Quantise the token at position lens[b]-1 (k_new, v_new [B,Hkv,D]) into 8-bit caches and decode with it in one
+    call: the same result and caches as aoh_kv_append_q8 + aoh_decode_q8."""
+    return _decode_q8(lib().aoh_decode_step_q8, (k_new, v_new), q, kv_full, kv_ring, head_is_streaming, lens, n_sink,
+                      window, out, workspace, stream)
+
+
+# ----------------------------------------------------------------------------- classifier
 
 def aoh_classify_workspace_bytes(n_layers, n_q_heads, n_kv_heads, d_head):
     return int(lib().aoh_classify_workspace_bytes(n_layers, n_q_heads, n_kv_heads, d_head))

@@ -21,12 +21,13 @@
 
 #include "aoh.h"
 #include "aoh_internal.h"
+#include "abi_host.h"
 
 using namespace aoh;
 
-namespace {
+namespace aoh {
 
-thread_local char g_err[512] = "";
+static thread_local char g_err[512] = "";
 
 aoh_status fail(aoh_status st, const char* fmt, ...) {
   va_list ap;
@@ -40,8 +41,6 @@ aoh_status ok() {
   g_err[0] = '\0';
   return AOH_OK;
 }
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Compute units of the current device, queried once per device (256 on an
 // MI355X, also the answer when the query fails).
@@ -57,7 +56,7 @@ int compute_units() {
   return n;
 }
 
-int elt_size(int dtype) { return dtype == AOH_BF16 ? 2 : 4; }
+static int elt_size(int dtype) { return dtype == AOH_BF16 ? 2 : 4; }
 
 // Checks a tensor descriptor: rank, dtype, positive sizes, unit last stride,
 // positive strides, alignment of the base pointer and strides for 16-byte
@@ -81,16 +80,6 @@ aoh_status check_tensor(const aoh_tensor* t, const char* name, int ndim, int dty
       return fail(AOH_ERR_INVALID_ARG, "%s: stride %d must be a multiple of %lld elements", name, i, (long long)vec);
   return AOH_OK;
 }
-
-// Head-scheduling pass: KV-head lists by label (ascending id) and each KV
-// head's rank inside its cache.
-struct HeadSchedule {
-  int n_ret = 0, n_str = 0;
-  uint8_t ret[kMaxKvHeads];
-  uint8_t str[kMaxKvHeads];
-  uint8_t rank[kMaxKvHeads];
-  uint64_t streaming_mask = 0;
-};
 
 aoh_status schedule_heads(const uint8_t* head_is_streaming, int hkv, HeadSchedule* hs) {
   if (!head_is_streaming) return fail(AOH_ERR_INVALID_ARG, "head_is_streaming: null pointer");
@@ -116,6 +105,45 @@ aoh_status check_mask_params(int n_sink, int window) {
   if ((int64_t)n_sink + window > (1ll << 30)) return fail(AOH_ERR_UNSUPPORTED, "n_sink + window too large");
   return AOH_OK;
 }
+
+aoh_status check_paged(const aoh_paged_cache* c, int n_ret, int64_t B) {
+  if (!n_ret) return AOH_OK;
+  if (!c) return fail(AOH_ERR_INVALID_ARG, "kv_full is null but %d retrieval heads exist", n_ret);
+  if (!c->k || !c->v || !c->block_table) return fail(AOH_ERR_INVALID_ARG, "kv_full: null pointer");
+  if (c->n_heads != n_ret)
+    return fail(AOH_ERR_INVALID_ARG, "kv_full.n_heads=%d but the mask has %d retrieval heads", c->n_heads, n_ret);
+  if (c->num_pages < 1 || c->max_pages_per_seq < 1) return fail(AOH_ERR_INVALID_ARG, "kv_full: empty cache");
+  if (c->num_pages > (1ll << 31) - 1) return fail(AOH_ERR_UNSUPPORTED, "kv_full: too many pages");
+  if ((int64_t)c->max_pages_per_seq * kPageTokens > (1ll << 30)) return fail(AOH_ERR_UNSUPPORTED, "kv_full: too many pages per sequence");
+  if (c->n_seqs < B)
+    return fail(AOH_ERR_INVALID_ARG, "kv_full.n_seqs=%d: the block table has fewer rows than the %lld sequences",
+                c->n_seqs, (long long)B);
+  if (reinterpret_cast<uintptr_t>(c->k) % 16 || reinterpret_cast<uintptr_t>(c->v) % 16)
+    return fail(AOH_ERR_INVALID_ARG, "kv_full: cache pointers must be 16-byte aligned");
+  if (c->v_token_major != 0 && c->v_token_major != 1)
+    return fail(AOH_ERR_INVALID_ARG, "kv_full.v_token_major=%d; must be 0 or 1", c->v_token_major);
+  return AOH_OK;
+}
+
+aoh_status check_ring(const aoh_ring_cache* c, int n_str, int n_sink, int window, int64_t B) {
+  if (!n_str) return AOH_OK;
+  if (!c) return fail(AOH_ERR_INVALID_ARG, "kv_ring is null but %d streaming heads exist", n_str);
+  if (!c->k || !c->v) return fail(AOH_ERR_INVALID_ARG, "kv_ring: null pointer");
+  if (c->n_heads != n_str)
+    return fail(AOH_ERR_INVALID_ARG, "kv_ring.n_heads=%d but the mask has %d streaming heads", c->n_heads, n_str);
+  if (c->capacity != n_sink + window)
+    return fail(AOH_ERR_INVALID_ARG, "kv_ring.capacity=%d must equal n_sink + window = %d", c->capacity, n_sink + window);
+  if (c->batch < B)
+    return fail(AOH_ERR_INVALID_ARG, "kv_ring.batch=%d: the ring holds fewer than the %lld sequences", c->batch,
+                (long long)B);
+  if (reinterpret_cast<uintptr_t>(c->k) % 16 || reinterpret_cast<uintptr_t>(c->v) % 16)
+    return fail(AOH_ERR_INVALID_ARG, "kv_ring: cache pointers must be 16-byte aligned");
+  return AOH_OK;
+}
+
+}  // namespace aoh
+
+namespace {
 
 // Decode split plan from the cache capacity.  A paged split is
 // split_blocks_full 16-token blocks (even, so a wave always reads whole
@@ -218,9 +246,7 @@ int32_t aoh_version(void) { return 100; }
 
 const char* aoh_last_error(void) { return g_err; }
 
-static aoh_status check_paged(const aoh_paged_cache* c, int n_ret, int64_t B);
 static aoh_status check_v_dim_major(const aoh_paged_cache* c, int n_ret, const char* call);
-static aoh_status check_ring(const aoh_ring_cache* c, int n_str, int n_sink, int window, int64_t B);
 
 // Prefill; with append set, also writes the prompt's K/V (positions 0..T-1 of
 // every sequence) into kv_full / kv_ring.
@@ -446,47 +472,12 @@ aoh_status aoh_prefill_append(const aoh_tensor* q, const aoh_tensor* k, const ao
   return prefill_impl(q, k, v, head_is_streaming, n_sink, window, chunk, true, kv_full, kv_ring, out, stream);
 }
 
-static aoh_status check_paged(const aoh_paged_cache* c, int n_ret, int64_t B) {
-  if (!n_ret) return AOH_OK;
-  if (!c) return fail(AOH_ERR_INVALID_ARG, "kv_full is null but %d retrieval heads exist", n_ret);
-  if (!c->k || !c->v || !c->block_table) return fail(AOH_ERR_INVALID_ARG, "kv_full: null pointer");
-  if (c->n_heads != n_ret)
-    return fail(AOH_ERR_INVALID_ARG, "kv_full.n_heads=%d but the mask has %d retrieval heads", c->n_heads, n_ret);
-  if (c->num_pages < 1 || c->max_pages_per_seq < 1) return fail(AOH_ERR_INVALID_ARG, "kv_full: empty cache");
-  if (c->num_pages > (1ll << 31) - 1) return fail(AOH_ERR_UNSUPPORTED, "kv_full: too many pages");
-  if ((int64_t)c->max_pages_per_seq * kPageTokens > (1ll << 30)) return fail(AOH_ERR_UNSUPPORTED, "kv_full: too many pages per sequence");
-  if (c->n_seqs < B)
-    return fail(AOH_ERR_INVALID_ARG, "kv_full.n_seqs=%d: the block table has fewer rows than the %lld sequences",
-                c->n_seqs, (long long)B);
-  if (reinterpret_cast<uintptr_t>(c->k) % 16 || reinterpret_cast<uintptr_t>(c->v) % 16)
-    return fail(AOH_ERR_INVALID_ARG, "kv_full: cache pointers must be 16-byte aligned");
-  if (c->v_token_major != 0 && c->v_token_major != 1)
-    return fail(AOH_ERR_INVALID_ARG, "kv_full.v_token_major=%d; must be 0 or 1", c->v_token_major);
-  return AOH_OK;
-}
-
 // Token-major V pages are written by aoh_kv_append and read by the reuse layer
 // only; the other readers and writers take dimension-major pages.
 static aoh_status check_v_dim_major(const aoh_paged_cache* c, int n_ret, const char* call) {
   if (n_ret && c->v_token_major)
     return fail(AOH_ERR_UNSUPPORTED, "%s needs dimension-major V pages (kv_full.v_token_major=0); "
                 "token-major pages are for aoh_kv_append and aoh_decode_reuse", call);
-  return AOH_OK;
-}
-
-static aoh_status check_ring(const aoh_ring_cache* c, int n_str, int n_sink, int window, int64_t B) {
-  if (!n_str) return AOH_OK;
-  if (!c) return fail(AOH_ERR_INVALID_ARG, "kv_ring is null but %d streaming heads exist", n_str);
-  if (!c->k || !c->v) return fail(AOH_ERR_INVALID_ARG, "kv_ring: null pointer");
-  if (c->n_heads != n_str)
-    return fail(AOH_ERR_INVALID_ARG, "kv_ring.n_heads=%d but the mask has %d streaming heads", c->n_heads, n_str);
-  if (c->capacity != n_sink + window)
-    return fail(AOH_ERR_INVALID_ARG, "kv_ring.capacity=%d must equal n_sink + window = %d", c->capacity, n_sink + window);
-  if (c->batch < B)
-    return fail(AOH_ERR_INVALID_ARG, "kv_ring.batch=%d: the ring holds fewer than the %lld sequences", c->batch,
-                (long long)B);
-  if (reinterpret_cast<uintptr_t>(c->k) % 16 || reinterpret_cast<uintptr_t>(c->v) % 16)
-    return fail(AOH_ERR_INVALID_ARG, "kv_ring: cache pointers must be 16-byte aligned");
   return AOH_OK;
 }
 
@@ -671,6 +662,7 @@ static aoh_status decode_impl(const aoh_tensor* q, const aoh_paged_cache* kv_ful
   a.lens = lens;
   a.B = (int)B; a.Hq = (int)Hq; a.gs = gs;
   a.ring_cap = ring_cap;
+  a.empty = std::nanf("");
   a.scale = (float)(1.0 / std::sqrt((double)D));
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)D));
   if (hs.n_ret) {
@@ -809,6 +801,7 @@ static aoh_status decode_impl(const aoh_tensor* q, const aoh_paged_cache* kv_ful
   // reuse: a retrieval head's "length" is its number of borrowed entries
   m.max_len = x.mode == kReuse ? x.top_k : max_pages * kPageTokens;
   m.ring_cap = ring_cap;
+  m.empty = a.empty;
   m.many_wgs = a.many_wgs;
   m.ws_cu = a.ws_cu; m.ws_n_ret = hs.n_ret; m.ws_n_str = hs.n_str; m.ws_items = a.ws_items;
   m.streaming_mask = hs.streaming_mask;

@@ -64,6 +64,7 @@ struct CacheView {
   int32_t n_groups;             // workgroups per (batch, KV head): ceil(n_splits / kSplitWaves)
   int32_t n_items;              // workgroups of the launch: B * n_kv * n_groups
   int32_t v_token_major;        // paged: V pages [16][D] (read by the reuse layer only)
+  const uint8_t* scales;        // 8-bit caches: scale bytes (K, V) of every row of a unit
   uint8_t kv_heads[kMaxKvHeads];  // KV head ids; rank in the cache = index here
 };
 
@@ -99,6 +100,7 @@ struct DecodeArgs {
   int64_t o_sb, o_sh;
   int32_t out_f32;
   float* ml_out;
+  float empty;                  // output of a sequence without tokens (work-space passes)
   float scale_log2;
   float scale;
   CacheView full;
@@ -144,6 +146,7 @@ struct MergeArgs {
   int32_t ws_cu, ws_n_ret, ws_n_str;
   const int32_t* ws_items;
   int32_t many_wgs;             // > 0: partials of decode_many_kernel
+  float empty;                  // output of an item without partials (work-space pass)
   uint64_t streaming_mask;      // bit g set = KV head g streaming
   float* ml_out;                // anchor layer: final (m, l) of each paged-cache head, [B][Hq][2]
 };
@@ -174,6 +177,39 @@ struct AppendArgs {
   uint64_t streaming_mask;
   uint8_t rank[kMaxKvHeads];    // rank of each KV head inside its cache
 };
+
+// Formats of the 8-bit caches (aoh_dtype values), and the bound on positions.
+constexpr int kFormatE4m3 = 2, kFormatI8 = 3;
+constexpr int kMaxPos = 1 << 30;
+
+// Writing tokens into the 8-bit caches, or reading them back into k / v.
+struct Q8Args {
+  const void* k;                // [B][n][Hkv][D], or packed [total][Hkv][D] (cu_seqlens; *_sb = 0)
+  const void* v;
+  int64_t k_sb, k_st, k_sh;
+  int64_t v_sb, v_st, v_sh;
+  const int32_t* start_pos;     // device [B]; nullptr: 0
+  const int32_t* cu_seqlens;    // writing packed tokens: device [B + 1]
+  const int32_t* lens;          // reading: device [B]
+  int32_t total;                // packed rows
+  int32_t B, n, Hkv;            // n: tokens of a sequence, at most
+  uint8_t* pk;                  // paged cache
+  uint8_t* pv;
+  uint8_t* ps;
+  const int32_t* block_table;
+  int32_t max_pages, num_pages, n_ret;
+  uint8_t* rk;                  // rings
+  uint8_t* rv;
+  uint8_t* rs;
+  int32_t n_str, ring_blocks;
+  int32_t n_sink, window;
+  int32_t chunk0;               // first 16-position chunk of the launch
+  uint64_t streaming_mask;
+  uint8_t rank[kMaxKvHeads];
+};
+hipError_t launch_q8(const Q8Args& a, int dtype, int format, int d, bool write, hipStream_t s);
+// Split pass of a decode step over the 8-bit caches (a.ws_cu, a.many_wgs as in launch_decode_split).
+hipError_t launch_decode_q8_split(const DecodeArgs& a, int d, int format, hipStream_t s);
 
 // The head classifier over L layers.  Weights are bf16 [L][H * D][d_model]
 // slices (layer stride *_sl, row stride *_sr, unit column stride).

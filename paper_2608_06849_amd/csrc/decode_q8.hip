@@ -1,0 +1,312 @@
+// Single-token decode over the 8-bit caches (layout and codes: q8.h; ranges,
+// merging and output: decode_split.h).
+//
+// A wave takes the blocks of its range four at a time (64 tokens, 16 KB at
+// d_head 128), the next four loading while it folds these:
+//   S^T[16 tokens x 16 heads] = K[16 x 32 dims] . Q^T       (D/32 steps a block)
+//   O^T[16 dims x 16 heads]  += V^T[16 dims x 32 tokens] . P^T   (D/16 a block pair)
+// with v_mfma_f32_16x16x32_bf16 on codes converted to bf16, exactly.  K's row
+// scale multiplies the scores (with log2(e) / sqrt(D)) and V's the
+// probabilities, where it is exact too: a probability is rounded to bf16, as in
+// the bf16 caches' pass, or for fp32 outputs kept as the sum of two bf16 numbers
+// (2^-17 of itself), which costs a second product.
+//   Lane group G = lane / 16 receives the scores of rows 4G .. 4G + 3 of a block,
+// and the k index of the second product is ordered so that it needs just those: P^T
+// stays in its lanes, and the V operand of dimension block 4j + n is word n of two
+// tiles (one of each block of the pair).  Row m of that operand is dimension
+// 64 j + 4 m + n, so the lane's sums are transposed in registers at the end.
+//   All addresses of a load are one uniform base and a constant offset of
+// the lane.  Block table entries are loaded 64 at a time, one a lane.
+#include <cfloat>
+
+#include "aoh_internal.h"
+#include "decode_split.h"
+#include "q8.h"
+
+namespace aoh {
+
+namespace {
+
+constexpr int kBlocks = 4;  // blocks a wave folds at a time
+
+// Codes and scales of kBlocks blocks.
+template <int D>
+struct Q8Chunk {
+  u32x4 k[kBlocks][D / 64];
+  u32x4 v[kBlocks][D / 64];
+  u32x2 s[kBlocks];
+};
+
+// Stores the step's token (position len - 1 of sequence b, KV head g) as row
+// `row` of a unit: lane t has D / 64 dimensions of K and of V.
+template <int D, bool I8>
+__device__ __forceinline__ void store_token(const DecodeArgs& a, uint8_t* uk, uint8_t* uv, uint8_t* us, int b, int g,
+                                            int row) {
+  constexpr int kPer = D / kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  uint32_t byte[2];
+  uint32_t code[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint16_t* p = t == 0 ? reinterpret_cast<const uint16_t*>(a.k_new) + (int64_t)b * a.kn_sb + (int64_t)g * a.kn_sh
+                               : reinterpret_cast<const uint16_t*>(a.v_new) + (int64_t)b * a.vn_sb + (int64_t)g * a.vn_sh;
+    float x[4] = {};
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      x[i] = bf16_to_f32(p[kPer * lane + i]);
+      amax = max(amax, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
+    }
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, kWave));
+    byte[t] = scale_byte<I8>(amax);
+    code[t] = to_codes<I8>(x, inverse_scale(byte[t]), byte[t] == 255u);
+  }
+  if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(uk + row * D + 2 * lane) = (uint16_t)code[0];
+  else uk[row * D + lane] = (uint8_t)code[0];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) uv[v_offset(kPer * lane + i, row)] = (uint8_t)(code[1] >> (8 * i));
+  if (lane == 0) *reinterpret_cast<uint16_t*>(us + 2 * row) = (uint16_t)(byte[0] | (byte[1] << 8));
+}
+
+}  // namespace
+
+template <int D, bool I8>
+struct Q8Body {
+  static constexpr int kD = D;
+  static constexpr bool kScores = false;
+  static __device__ __forceinline__ int dim(int t, int G) { return 64 * (t >> 2) + 16 * G + 4 * (t & 3); }
+
+  // Folds the blocks c .. c + kBlocks - 1 of a cache row (rows from tok_end on are masked).
+  static __device__ __forceinline__ void fold(const DecodeArgs& a, Q8Chunk<D>& x, const bf16x8 (&q)[D / 32], int c,
+                                              int tok_end, f32x4 (&acc)[D / 16], float& m_run, float& l_run) {
+    const int G = (threadIdx.x & (kWave - 1)) >> 4;
+    const bool partial = (c + kBlocks) * kPage > tok_end;
+    const int left = tok_end - c * kPage - 4 * G;  // rows of this lane group, from its first one
+    float s[kBlocks][4], vs[kBlocks][4];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int X = 0; X < kBlocks; ++X) {
+      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        sc = mfma16(codes_operand<I8>(x.k[X][i][0], x.k[X][i][1]), q[2 * i], sc);
+        sc = mfma16(codes_operand<I8>(x.k[X][i][2], x.k[X][i][3]), q[2 * i + 1], sc);
+      }
+      const float ks[4] = {scale_of<0>(x.s[X][0]), scale_of<16>(x.s[X][0]), scale_of<0>(x.s[X][1]), scale_of<16>(x.s[X][1])};
+      vs[X][0] = scale_of<8>(x.s[X][0]);
+      vs[X][1] = scale_of<24>(x.s[X][0]);
+      vs[X][2] = scale_of<8>(x.s[X][1]);
+      vs[X][3] = scale_of<24>(x.s[X][1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[X][i] = sc[i] * ks[i] * a.scale_log2;
+        if (partial && 16 * X + i >= left) {
+          // rows past the end may hold anything: weight 0, and no factor that is not finite
+          s[X][i] = -INFINITY;
+          vs[X][i] = 0.f;
+        }
+        mx = fmaxf(mx, s[X][i]);
+      }
+    }
+    mx = wave_xor_max(mx, 16);
+    mx = xor32_max(mx);
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = fast_exp2(m_run - m_new);
+    m_run = m_new;
+    float psum = 0.f;
+    bf16x8 w[kBlocks / 2];
+#pragma unroll
+    for (int X = 0; X < kBlocks; ++X)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = fast_exp2(s[X][i] - m_new);
+        psum += p;
+        s[X][i] = p * vs[X][i];
+        w[X / 2][4 * (X & 1) + i] = f32_to_bf16(s[X][i]);
+      }
+    l_run = l_run * alpha + psum;
+    if (partial) {
+#pragma unroll
+      for (int X = 0; X < kBlocks; ++X) {
+        const int n = min(max(left - 16 * X, 0), 4);
+        const uint32_t keep = n == 4 ? ~0u : (1u << (8 * n)) - 1u;  // codes past the end may be NaN
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.v[X][j][e] &= keep;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
+    add(x, w, acc);
+    if (a.out_f32) {
+      // what the first rounding left of the weights
+#pragma unroll
+      for (int X = 0; X < kBlocks; ++X)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 4 * (X & 1) + i;
+          w[X / 2][e] = f32_to_bf16(s[X][i] - (float)w[X / 2][e]);
+        }
+      add(x, w, acc);
+    }
+  }
+
+  // acc += V^T . W^T for the weights of a chunk's block pairs.
+  static __device__ __forceinline__ void add(const Q8Chunk<D>& x, const bf16x8 (&w)[kBlocks / 2], f32x4 (&acc)[D / 16]) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int P = 0; P < kBlocks / 2; ++P)
+        acc[t] = mfma16(codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]), w[P], acc[t]);
+  }
+
+  template <bool RING>
+  static __device__ __forceinline__ void run(const DecodeArgs& a, const CacheView& cv, int b, int kvl, int len,
+                                             int blk0, int blk_lim, f32x4 (&out)[D / 16], float& m_out, float& l_out,
+                                             void*) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int col = lane & 15, G = lane >> 4;
+    const int g = cv.kv_heads[kvl];
+    // Lengths beyond the cache capacity are clamped so no read leaves the cache.
+    const int n_valid = RING ? min(len, a.ring_cap) : min(len, cv.max_pages * kPage);
+    const int blk_end = min(blk_lim, (n_valid + kPage - 1) / kPage);
+    if (blk0 >= blk_end) return;
+    const int tok_end = min(n_valid, blk_end * kPage);
+
+    // Block table entries of the 64 blocks from `first` on, one a lane.
+    const int32_t* bt = RING ? nullptr : cv.block_table + (int64_t)b * cv.max_pages;
+    auto entries = [&](int first) -> int { return RING ? 0 : bt[min(first + lane, blk_end - 1)]; };
+    const int64_t ring0 = RING ? ((int64_t)b * cv.n_kv + kvl) * cv.ring_blocks : 0;
+    // An invalid entry reads page 0, never outside the cache.
+    auto unit_of = [&](int blk, int first, int ent) -> int64_t {
+      if (RING) return ring0 + blk;
+      const int e = __builtin_amdgcn_readlane(ent, blk - first);
+      return (int64_t)((e < 0 || e >= cv.num_pages) ? 0 : e) * cv.n_kv + kvl;
+    };
+    int first = blk0;
+    int ent = entries(first);
+
+    // Q^T operand: column = query head, dimensions in the order of the K loads.
+    bf16x8 q[D / 32];
+    {
+      const uint16_t* qp = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)b * a.q_sb + (int64_t)(g * a.gs + col) * a.q_sh;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 w = {0u, 0u, 0u, 0u};
+          if (col < a.gs) w = ld16(qp + 64 * i + 16 * G + 8 * h);
+          q[2 * i + h] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+
+    const uint8_t* ck = reinterpret_cast<const uint8_t*>(cv.k);
+    const uint8_t* cvv = reinterpret_cast<const uint8_t*>(cv.v);
+    if (a.k_new) {
+      // Fused step: the wave whose range holds the token's block stores it before
+      // it reads the block; no other wave reads this unit.
+      const int p = len - 1;
+      const int slot = RING ? (p < a.n_sink ? p : a.n_sink + (p - a.n_sink) % a.window) : p;
+      const int blk = slot / kPage;
+      if (blk >= blk0 && blk < blk_end) {
+        int64_t unit = -1;
+        if (RING) {
+          unit = ring0 + blk;
+        } else {
+          const int page = __builtin_amdgcn_readfirstlane(bt[blk]);
+          if (page >= 0 && page < cv.num_pages) unit = (int64_t)page * cv.n_kv + kvl;
+        }
+        if (unit >= 0) {
+          store_token<D, I8>(a, const_cast<uint8_t*>(ck) + unit * (kPage * D), const_cast<uint8_t*>(cvv) + unit * (kPage * D),
+                             const_cast<uint8_t*>(cv.scales) + unit * kScaleBytes, b, g, slot % kPage);
+          // The stores must reach the cache before this wave's loads of it.
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+      }
+    }
+
+    const int k_off = col * D + 16 * G;   // K row `col`, 64 bytes of it a load
+    const int v_off = col * 64 + 16 * G;  // V tile (dimension quad col, rows 4G .. 4G + 3)
+    auto load_block = [&](Q8Chunk<D>& x, int X, int blk) {
+      const int64_t u = unit_of(blk, first, ent);
+      const uint8_t* kb = ck + u * (kPage * D);
+      const uint8_t* vb = cvv + u * (kPage * D);
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        x.k[X][i] = ld16_stream(kb + k_off + 64 * i);
+        x.v[X][i] = ld16_stream(vb + v_off + 1024 * i);
+      }
+      x.s[X] = ld8(cv.scales + u * kScaleBytes + 8 * G);
+    };
+    // Blocks c .. c + kBlocks - 1; what lies past the end stays as it is (masked).
+    auto load = [&](Q8Chunk<D>& x, int c) {
+      if (!RING && c + kBlocks > first + kWave) {  // 64 - kBlocks blocks further at the earliest
+        first = c;
+        ent = entries(first);
+      }
+#pragma unroll
+      for (int X = 0; X < kBlocks; ++X)
+        if (c + X < blk_end) load_block(x, X, c + X);
+    };
+
+    f32x4 acc[D / 16];
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Finite, so that tokens whose score is -inf have weight 0 however the range is cut.
+    float m_run = -FLT_MAX, l_run = 0.f;
+
+    Q8Chunk<D> x, y;
+#pragma unroll
+    for (int X = 0; X < kBlocks; ++X) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) x.k[X][i] = x.v[X][i] = y.k[X][i] = y.v[X][i] = u32x4{0u, 0u, 0u, 0u};
+      x.s[X] = y.s[X] = u32x2{0u, 0u};
+    }
+    load(x, blk0);
+    for (int c = blk0; c < blk_end; c += 2 * kBlocks) {
+      if (c + kBlocks < blk_end) load(y, c + kBlocks);
+      fold(a, x, q, c, tok_end, acc, m_run, l_run);
+      if (c + kBlocks >= blk_end) break;
+      if (c + 2 * kBlocks < blk_end) load(x, c + 2 * kBlocks);
+      fold(a, y, q, c + kBlocks, tok_end, acc, m_run, l_run);
+    }
+
+    // acc[4j + n][i]: dimension 64 j + 16 G + 4 i + n
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) out[t][n] = acc[(t & ~3) + n][t & 3];
+    float l_tot = wave_xor_sum(l_run, 16);
+    l_tot = xor32_sum(l_tot);
+    m_out = m_run;
+    l_out = l_tot;
+  }
+};
+
+namespace {
+
+template <class Body>
+void launch_body(const DecodeArgs& a, hipStream_t s) {
+  const dim3 blk(kSplitWaves * kWave);
+  if (a.many_wgs) hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), blk, 0, s, a);
+  else hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), blk, 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_decode_q8_split(const DecodeArgs& a, int d, int format, hipStream_t s) {
+  if (d == 64) {
+    if (format == kFormatI8) launch_body<Q8Body<64, true>>(a, s);
+    else launch_body<Q8Body<64, false>>(a, s);
+  } else {
+    if (format == kFormatI8) launch_body<Q8Body<128, true>>(a, s);
+    else launch_body<Q8Body<128, false>>(a, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace aoh
