@@ -77,14 +77,10 @@ struct Q8Body {
   static constexpr bool kScores = false;
   static __device__ __forceinline__ int dim(int t, int G) { return 64 * (t >> 2) + 16 * G + 4 * (t & 3); }
 
-  // Folds the blocks c .. c + kBlocks - 1 of a cache row (rows from tok_end on are masked).
-  static __device__ __forceinline__ void fold(const DecodeArgs& a, Q8Chunk<D>& x, const bf16x8 (&q)[D / 32], int c,
-                                              int tok_end, f32x4 (&acc)[D / 16], float& m_run, float& l_run) {
-    const int G = (threadIdx.x & (kWave - 1)) >> 4;
-    const bool partial = (c + kBlocks) * kPage > tok_end;
-    const int left = tok_end - c * kPage - 4 * G;  // rows of this lane group, from its first one
-    float s[kBlocks][4], vs[kBlocks][4];
-    float mx = -INFINITY;
+  // Scores of the blocks c .. c + kBlocks - 1 of a cache row (rows from `left` on,
+  // counted from the lane group's first one, get -inf) and V's scales.
+  static __device__ __forceinline__ void scores(const DecodeArgs& a, const Q8Chunk<D>& x, const bf16x8 (&q)[D / 32],
+                                                bool partial, int left, float (&s)[kBlocks][4], float (&vs)[kBlocks][4]) {
 #pragma unroll
     for (int X = 0; X < kBlocks; ++X) {
       f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -106,24 +102,34 @@ struct Q8Body {
           s[X][i] = -INFINITY;
           vs[X][i] = 0.f;
         }
-        mx = fmaxf(mx, s[X][i]);
       }
     }
+  }
+
+  // Folds scores and V codes of kBlocks blocks into the running softmax state.
+  static __device__ __forceinline__ void fold(const DecodeArgs& a, Q8Chunk<D>& x, float (&s)[kBlocks][4],
+                                              const float (&vs)[kBlocks][4], bool partial, int left,
+                                              f32x4 (&acc)[D / 16], float& m_run, float& l_run) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 4 * kBlocks; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
     mx = wave_xor_max(mx, 16);
     mx = xor32_max(mx);
     const float m_new = fmaxf(m_run, mx);
     const float alpha = fast_exp2(m_run - m_new);
     m_run = m_new;
     float psum = 0.f;
-    bf16x8 w[kBlocks / 2];
+    bf16x8 w[kBlocks / 2], r[kBlocks / 2];
 #pragma unroll
     for (int X = 0; X < kBlocks; ++X)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float p = fast_exp2(s[X][i] - m_new);
         psum += p;
-        s[X][i] = p * vs[X][i];
-        w[X / 2][4 * (X & 1) + i] = f32_to_bf16(s[X][i]);
+        const float pv = p * vs[X][i];
+        const bf16 h = f32_to_bf16(pv);
+        w[X / 2][4 * (X & 1) + i] = h;
+        r[X / 2][4 * (X & 1) + i] = f32_to_bf16(pv - (float)h);
       }
     l_run = l_run * alpha + psum;
     if (partial) {
@@ -141,27 +147,15 @@ struct Q8Body {
     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
-    add(x, w, acc);
-    if (a.out_f32) {
-      // what the first rounding left of the weights
-#pragma unroll
-      for (int X = 0; X < kBlocks; ++X)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 4 * (X & 1) + i;
-          w[X / 2][e] = f32_to_bf16(s[X][i] - (float)w[X / 2][e]);
-        }
-      add(x, w, acc);
-    }
-  }
-
-  // acc += V^T . W^T for the weights of a chunk's block pairs.
-  static __device__ __forceinline__ void add(const Q8Chunk<D>& x, const bf16x8 (&w)[kBlocks / 2], f32x4 (&acc)[D / 16]) {
+    // acc += V^T . (w + what rounding left of the weights)^T
 #pragma unroll
     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-      for (int P = 0; P < kBlocks / 2; ++P)
-        acc[t] = mfma16(codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]), w[P], acc[t]);
+      for (int P = 0; P < kBlocks / 2; ++P) {
+        const bf16x8 v = codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]);
+        acc[t] = mfma16(v, w[P], acc[t]);
+        acc[t] = mfma16(v, r[P], acc[t]);
+      }
   }
 
   template <bool RING>
@@ -231,27 +225,35 @@ struct Q8Body {
 
     const int k_off = col * D + 16 * G;   // K row `col`, 64 bytes of it a load
     const int v_off = col * 64 + 16 * G;  // V tile (dimension quad col, rows 4G .. 4G + 3)
-    auto load_block = [&](Q8Chunk<D>& x, int X, int blk) {
-      const int64_t u = unit_of(blk, first, ent);
-      const uint8_t* kb = ck + u * (kPage * D);
-      const uint8_t* vb = cvv + u * (kPage * D);
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        x.k[X][i] = ld16_stream(kb + k_off + 64 * i);
-        x.v[X][i] = ld16_stream(vb + v_off + 1024 * i);
-      }
-      x.s[X] = ld8(cv.scales + u * kScaleBytes + 8 * G);
-    };
     // Blocks c .. c + kBlocks - 1; what lies past the end stays as it is (masked).
-    auto load = [&](Q8Chunk<D>& x, int c) {
-      if (!RING && c + kBlocks > first + kWave) {  // 64 - kBlocks blocks further at the earliest
-        first = c;
-        ent = entries(first);
-      }
+    // K and V of a chunk are loaded into the registers of the chunk before it, each
+    // as soon as those are used up.
+    Q8Chunk<D> x;
+    auto load_k = [&](int c) {
 #pragma unroll
-      for (int X = 0; X < kBlocks; ++X)
-        if (c + X < blk_end) load_block(x, X, c + X);
+      for (int X = 0; X < kBlocks; ++X) {
+        if (c + X >= blk_end) break;
+        const int64_t u = unit_of(c + X, first, ent);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) x.k[X][i] = ld16_stream(ck + u * (kPage * D) + k_off + 64 * i);
+        x.s[X] = ld8(cv.scales + u * kScaleBytes + 8 * G);
+      }
     };
+    auto load_v = [&](int c) {
+#pragma unroll
+      for (int X = 0; X < kBlocks; ++X) {
+        if (c + X >= blk_end) break;
+        const int64_t u = unit_of(c + X, first, ent);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) x.v[X][i] = ld16_stream(cvv + u * (kPage * D) + v_off + 1024 * i);
+      }
+    };
+#pragma unroll
+    for (int X = 0; X < kBlocks; ++X) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) x.k[X][i] = x.v[X][i] = u32x4{0u, 0u, 0u, 0u};
+      x.s[X] = u32x2{0u, 0u};
+    }
 
     f32x4 acc[D / 16];
 #pragma unroll
@@ -259,20 +261,23 @@ struct Q8Body {
     // Finite, so that tokens whose score is -inf have weight 0 however the range is cut.
     float m_run = -FLT_MAX, l_run = 0.f;
 
-    Q8Chunk<D> x, y;
-#pragma unroll
-    for (int X = 0; X < kBlocks; ++X) {
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) x.k[X][i] = x.v[X][i] = y.k[X][i] = y.v[X][i] = u32x4{0u, 0u, 0u, 0u};
-      x.s[X] = y.s[X] = u32x2{0u, 0u};
-    }
-    load(x, blk0);
-    for (int c = blk0; c < blk_end; c += 2 * kBlocks) {
-      if (c + kBlocks < blk_end) load(y, c + kBlocks);
-      fold(a, x, q, c, tok_end, acc, m_run, l_run);
-      if (c + kBlocks >= blk_end) break;
-      if (c + 2 * kBlocks < blk_end) load(x, c + 2 * kBlocks);
-      fold(a, y, q, c + kBlocks, tok_end, acc, m_run, l_run);
+    load_k(blk0);
+    load_v(blk0);
+    for (int c = blk0; c < blk_end; c += kBlocks) {
+      const bool partial = (c + kBlocks) * kPage > tok_end;
+      const int left = tok_end - c * kPage - 4 * G;
+      float s[kBlocks][4], vs[kBlocks][4];
+      scores(a, x, q, partial, left, s, vs);
+      const int next = c + kBlocks;
+      if (next < blk_end) {
+        if (!RING && next + kBlocks > first + kWave) {  // entries of 64 - kBlocks blocks and more were used
+          first = next;
+          ent = entries(first);
+        }
+        load_k(next);
+      }
+      fold(a, x, s, vs, partial, left, acc, m_run, l_run);
+      if (next < blk_end) load_v(next);
     }
 
     // acc[4j + n][i]: dimension 64 j + 16 G + 4 i + n
