@@ -77,6 +77,11 @@ __device__ __forceinline__ void store8(float* p, u32x2 w, float scale) {
   }
 }
 
+// 2^E of a scale byte, NaN for 255.
+__device__ __forceinline__ float row_scale(uint32_t byte) {
+  return __builtin_bit_cast(float, byte == 255u ? 0x7fc00000u : byte << 23);
+}
+
 // Codes and scale byte of the row that D / 8 neighbouring lanes hold.
 template <int D, bool I8>
 __device__ __forceinline__ u32x2 quantise8(const float (&x)[8], uint32_t& byte) {
@@ -234,9 +239,9 @@ __global__ __launch_bounds__(2 * D) void read_q8_kernel(Q8Args a) {
   if (on) {
     const int64_t t = p - start;
     store8<I8>(reinterpret_cast<T*>(const_cast<void*>(a.k)) + (int64_t)b * a.k_sb + t * a.k_st + (int64_t)g * a.k_sh + 8 * c,
-               kw, scale_of<0>(sw));
+               kw, row_scale(sw & 0xffu));
     store8<I8>(reinterpret_cast<T*>(const_cast<void*>(a.v)) + (int64_t)b * a.v_sb + t * a.v_st + (int64_t)g * a.v_sh + 8 * c,
-               vw, scale_of<8>(sw));
+               vw, row_scale(sw >> 8));
   }
 }
 

@@ -1,0 +1,252 @@
+"""Writing the 8-bit caches and reading them back (aoh_kv_append_q8, aoh_kv_append_q8_varlen, aoh_kv_read_q8) against
+the oracle's plain caches, bit for bit: codes, scale bytes, and every byte that must not change."""
+import numpy as np
+import pytest
+import torch
+
+import synth
+from oracle import q8
+from oracle.cache_model import ring_slot, split_heads
+from paper_2608_06849_amd import (AohError, PagedCacheQ8, RingCacheQ8, aoh_kv_append_q8, aoh_kv_append_q8_varlen,
+                                  aoh_kv_read_q8)
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF = torch.bfloat16
+DTYPES = {q8.E4M3: torch.float8_e4m3fn, q8.I8: torch.int8}
+POISON = 0xA5
+
+
+def raw(t):
+    return t.view(torch.uint8).cpu().numpy().copy()
+
+
+class Caches:
+    """Poisoned caches on the GPU, and the same bytes for the oracle."""
+
+    def __init__(self, fmt, labels, d, batch, pages, n_sink, window, seed, unmapped=()):
+        ret, strm = split_heads(labels)
+        self.fmt, self.labels, self.n_sink, self.window = fmt, labels, n_sink, window
+        table = synth.page_permutation(batch * pages, seed, "q8-pages").reshape(batch, pages).astype(np.int32)
+        for b, page in unmapped:
+            table[b, page] = (-1, batch * pages)[page % 2]
+        self.table = table
+        dt = DTYPES[fmt]
+        self.full = PagedCacheQ8.allocate(batch * pages, len(ret), d, dt, torch.from_numpy(table)) if ret else None
+        self.ring = RingCacheQ8.allocate(batch, len(strm), n_sink, window, d, dt) if strm else None
+        for c in (self.full, self.ring):
+            for t in (c.k, c.v, c.scales) if c else ():
+                t.view(torch.uint8).fill_(POISON)
+        self.want = [tuple(raw(t) for t in (c.k, c.v, c.scales)) if c else None for c in (self.full, self.ring)]
+
+    def append(self, k, v, starts, counts):
+        """What the oracle does with k, v [B][n][Hkv][D] (tensors)."""
+        q8.append(*self.want, self.table, k.double().cpu().numpy(), v.double().cpu().numpy(), self.labels, starts,
+                  counts, self.n_sink, self.window, self.fmt)
+
+    def check(self, what=""):
+        for c, want, name in zip((self.full, self.ring), self.want, ("paged", "ring")):
+            for t, w, part in zip((c.k, c.v, c.scales) if c else (), want or (), ("K", "V", "scales")):
+                assert np.array_equal(raw(t), w), f"{what}: {name} {part}"
+
+
+def rows(shape, seed, name, dtype=BF):
+    x = synth.gaussian(shape, seed, name) * np.exp2(np.random.default_rng(seed).integers(-6, 7, shape[:-1]))[..., None]
+    return torch.from_numpy(x.astype(np.float32)).to(dtype).to(DEV)
+
+
+def int32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+CASES = [  # labels, d, n_sink, window, starts, n
+    ([0], 128, 0, 1, [0], 1),
+    ([1], 64, 0, 1, [5], 3),
+    ([0, 1], 128, 4, 29, [3, 0, 40], 17),
+    ([1, 0, 0], 64, 16, 32, [0, 16, 33], 80),
+    ([0, 1, 1, 0, 1], 128, 16, 48, [15, 1, 64, 31], 65),
+    ([1, 1], 128, 5, 11, [0, 9, 1000], 15),
+    ([0, 0], 64, 0, 7, [7, 100], 16),
+]
+
+
+@pytest.mark.parametrize("fmt", [q8.E4M3, q8.I8])
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+@pytest.mark.parametrize("labels,d,n_sink,window,starts,n", CASES)
+def test_append_and_read(labels, d, n_sink, window, starts, n, dtype, fmt):
+    b, h, seed = len(starts), len(labels), 17 * n + d
+    pages = (max(starts) + 2 * n + 15) // 16
+    c = Caches(fmt, labels, d, b, pages, n_sink, window, seed)
+    # K and V are slices of one tensor; twice, so that an append meets rows that are there already
+    kv = rows((b, 2 * n, 2 * h, d), seed, "q8-kv", dtype)
+    for i in range(2):
+        k, v = kv[:, i * n:(i + 1) * n, :h], kv[:, i * n:(i + 1) * n, h:]
+        at = [s + i * n for s in starts]
+        aoh_kv_append_q8(k, v, labels, int32(at), c.full, c.ring, n_sink, window)
+        c.append(k, v, at, [n] * b)
+        c.check(f"append {i}")
+
+    # read the second half's range and a little around it into strided outputs of both types
+    first = [max(0, s + n - 3) for s in starts]
+    lens = [s + 2 * n for s in starts]
+    m = n + 9
+    want = q8.stored(kv.double().cpu().numpy(), fmt)
+    for out in (BF, torch.float32):
+        kv_out = torch.full((b, m, 2 * h, d), 7.0, dtype=out, device=DEV)
+        aoh_kv_read_q8(c.full, c.ring, labels, int32(first), int32(lens), n_sink, window, kv_out[:, :, :h], kv_out[:, :, h:])
+        got = kv_out.double().cpu().numpy()
+        for i in range(b):
+            for t in range(m):
+                p = first[i] + t
+                for g in range(2 * h):
+                    gone = labels[g % h] and n_sink <= p < lens[i] - window
+                    if p >= lens[i] or gone:
+                        assert (got[i, t, g] == 7.0).all(), (i, t, g)
+                    elif p >= starts[i]:  # rows before were never written
+                        assert np.array_equal(got[i, t, g], want[i, p - starts[i], g]), (i, t, g)
+
+
+@pytest.mark.parametrize("fmt", [q8.E4M3, q8.I8])
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_rows_at_the_edges_of_the_formats(fmt, dtype):
+    d, n = 64, 48
+    x = synth.gaussian((1, n, 2, d), 3, "q8-edge").astype(np.float32)
+    x[0, 0] = 0.0
+    x[0, 1, :, 5] = np.nan
+    x[0, 2, :, 6] = np.inf
+    x[0, 3, :, 7] = -np.inf
+    x[0, 4, :, 8] = 2.0 ** 127
+    x[0, 5, :, 9] = -1.9921875 * 2.0 ** 126
+    x[0, 6] = 2.0 ** -149                   # subnormal
+    x[0, 7] *= np.float32(2.0 ** -115)      # below the least scale
+    x[0, 8] *= np.float32(2.0 ** -98)
+    x[0, 9] *= np.float32(2.0 ** 120)
+    grid = np.sort(np.unique(q8.code_values(fmt)[np.isfinite(q8.code_values(fmt))]))
+    mid = (grid[1:] + grid[:-1]) / 2
+    for t in range(10, n):                  # ties at every code, exact in both input types where 8 bits hold them
+        x[0, t] = np.random.default_rng(t).choice(mid, (2, d)) * 2.0 ** (t - 20)
+        x[0, t, :, 0] = grid[-1] * 2.0 ** (t - 20)
+    k = torch.from_numpy(x).to(dtype).to(DEV)
+    v = k.flip(1).contiguous()
+    c = Caches(fmt, [0, 1], d, 1, 3, 16, 32, 5)
+    aoh_kv_append_q8(k, v, [0, 1], None, c.full, c.ring, 16, 32)
+    c.append(k, v, [0], [n])
+    c.check()
+    out = [torch.zeros((1, n, 2, d), dtype=torch.float32, device=DEV) for _ in range(2)]
+    aoh_kv_read_q8(c.full, c.ring, [0, 1], None, int32([n]), 16, 32, *out)
+    for o, i in zip(out, (k, v)):
+        assert np.array_equal(o.double().cpu().numpy(), q8.stored(i.double().cpu().numpy(), fmt), equal_nan=True)
+
+
+@pytest.mark.parametrize("fmt", [q8.E4M3, q8.I8])
+@pytest.mark.parametrize("out", [BF, torch.float32])
+def test_every_code_and_scale_reads_back(fmt, out):
+    # codes 0 .. 255 in two rows of 128 at each scale byte that an append writes (27 .. 248), and NaN rows
+    d, pages = 128, 32
+    full = PagedCacheQ8.allocate(pages, 1, d, DTYPES[fmt], torch.arange(pages, dtype=torch.int32).view(1, -1))
+    n = pages * 16
+    code = (np.arange(n)[:, None] % 2 * d + np.arange(d)).astype(np.uint8)
+    byte = np.where(np.arange(n) // 2 + 27 <= 248, np.arange(n) // 2 + 27, 255).astype(np.uint8)
+    # the largest codes times the largest scales pass the range of the types
+    full.k.view(torch.uint8).copy_(torch.from_numpy(code.reshape(pages, 1, 16, d)))
+    full.v.view(torch.uint8).copy_(torch.from_numpy(np.ascontiguousarray(q8.v_unit(code[::-1].reshape(pages, 1, 16, d)))))
+    full.scales.copy_(torch.from_numpy(np.stack([byte, byte[::-1]], -1).reshape(pages, 1, 16, 2)))
+    k, v = (torch.zeros((1, n, 1, d), dtype=out, device=DEV) for _ in range(2))
+    aoh_kv_read_q8(full, None, [0], None, int32([n]), 0, 1, k, v)
+    want = q8.values(code, byte, fmt)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    assert np.array_equal(k[0, :, 0].double().cpu().numpy(), want, equal_nan=True)
+    assert np.array_equal(v[0, ::1, 0].double().cpu().numpy(), want[::-1], equal_nan=True)
+
+
+def test_packed_tokens_equal_dense_ones():
+    # counts of 0, 1, 16 and others, start positions, a bound that cuts the longest
+    counts, starts, labels, d, n_sink, window = [0, 1, 16, 70, 33], [9, 15, 0, 5, 100], [0, 1, 0], 128, 4, 28
+    for max_new in (70, 40):
+        for with_start in (True, False):
+            at = starts if with_start else [0] * 5
+            c = Caches(q8.E4M3, labels, d, 5, 12, n_sink, window, 8)
+            k, v = (rows((sum(counts), 3, d), 8, f"q8-packed-{s}") for s in "kv")
+            cu = np.concatenate([[0], np.cumsum(counts)])
+            aoh_kv_append_q8_varlen(k, v, int32(cu.tolist()), max_new, labels, int32(at) if with_start else None, c.full,
+                                    c.ring, n_sink, window)
+            kd, vd = (torch.zeros((5, 70, 3, d), dtype=BF, device=DEV) for _ in range(2))
+            for b, n in enumerate(counts):
+                kd[b, :n], vd[b, :n] = k[cu[b]:cu[b + 1]], v[cu[b]:cu[b + 1]]
+            c.append(kd, vd, at, [min(n, max_new) for n in counts])
+            c.check(f"max_new {max_new}, start {with_start}")
+
+
+def test_packed_entries_are_clamped():
+    c = Caches(q8.I8, [0], 64, 3, 4, 0, 1, 9)
+    k = rows((20, 1, 64), 9, "q8-clamp")
+    # entries below 0 and beyond the tensor, and a sequence that ends before it starts
+    aoh_kv_append_q8_varlen(k, k, int32([-5, 12, 7, 900]), 64, [0], None, c.full, None, 0, 1)
+    kd = torch.zeros((3, 20, 1, 64), dtype=BF, device=DEV)
+    kd[0, :12], kd[2, :13] = k[:12], k[7:20]
+    c.append(kd, kd, [0, 0, 0], [12, 0, 13])
+    c.check()
+
+
+def test_positions_without_a_place():
+    # unmapped pages, positions beyond the table, start positions that are none
+    labels, d, n_sink, window = [0, 1], 64, 2, 30
+    c = Caches(q8.E4M3, labels, d, 4, 4, n_sink, window, 10, unmapped=[(0, 1), (1, 2)])
+    k, v = (rows((4, 50, 2, d), 10, f"q8-lost-{s}") for s in "kv")
+    starts = [3, 30, -1, 1 << 30]
+    aoh_kv_append_q8(k, v, labels, int32(starts), c.full, c.ring, n_sink, window)
+    c.append(k, v, starts, [50] * 4)
+    c.check()
+    out = [torch.full((4, 90, 2, d), 7.0, dtype=BF, device=DEV) for _ in range(2)]
+    aoh_kv_read_q8(c.full, c.ring, labels, int32([0, 0, -1, 1 << 30]), int32([53, 80, 60, 60]), n_sink, window, *out)
+    want = q8.stored(k.double().cpu().numpy(), q8.E4M3)
+    got = out[0].double().cpu().numpy()
+    assert np.array_equal(got[0, 3:16, 0], want[0, :13, 0]) and (got[0, 16:32, 0] == 7.0).all()
+    assert np.array_equal(got[0, 32:53, 0], want[0, 29:, 0]) and (got[0, 53:] == 7.0).all()
+    assert (got[1, 32:48, 0] == 7.0).all() and (got[1, 64:, 0] == 7.0).all()  # unmapped; beyond the table
+    assert np.array_equal(got[1, 50:80, 1], want[1, 20:, 1]) and (got[2:] == 7.0).all()
+
+
+def test_cache_of_more_than_4_gib():
+    # pages whose byte offsets pass 32 bits
+    pages, heads, d = (9 << 29) // (8 * 2048), 8, 128
+    assert pages * heads * 16 * d > 1 << 32
+    used = [0, pages // 2 + 1, pages - 1]
+    full = PagedCacheQ8.allocate(pages, heads, d, torch.int8, torch.tensor([used], dtype=torch.int32))
+    k, v = (rows((1, 48, heads, d), 12, f"q8-far-{s}") for s in "kv")
+    aoh_kv_append_q8(k, v, [0] * heads, None, full, None, 0, 1)
+    out = [torch.zeros_like(k) for _ in range(2)]
+    aoh_kv_read_q8(full, None, [0] * heads, None, int32([48]), 0, 1, *out)
+    for o, i in zip(out, (k, v)):
+        assert np.array_equal(o.double().cpu().numpy(), q8.stored(i.double().cpu().numpy(), q8.I8))
+    kc, _ = q8.quantise(k.double().cpu().numpy(), q8.I8)
+    assert np.array_equal(raw(full.k[pages - 1]), kc[0, 32:].transpose(1, 0, 2))
+
+
+def test_more_sequences_than_a_grid_dimension():
+    b, d = 65537, 64
+    table = torch.arange(b, dtype=torch.int32).view(b, 1)
+    full = PagedCacheQ8.allocate(b, 1, d, torch.int8, table)
+    k = torch.randn((b, 1, 1, d), dtype=BF, device=DEV)
+    start = torch.arange(b, dtype=torch.int32, device=DEV) % 16
+    aoh_kv_append_q8(k, k, [0], start, full, None, 0, 1)
+    out = [torch.zeros_like(k) for _ in range(2)]
+    aoh_kv_read_q8(full, None, [0], start, start + 1, 0, 1, *out)
+    want = q8.stored(k.double().cpu().numpy(), q8.I8)
+    for o in out:
+        assert np.array_equal(o.double().cpu().numpy(), want)
+
+
+def test_refused_calls_write_nothing():
+    c = Caches(q8.E4M3, [0, 1], 64, 2, 4, 2, 30, 11)
+    k = rows((2, 5, 2, 64), 11, "q8-no")
+    with pytest.raises(AohError):
+        aoh_kv_append_q8(k, k, [0, 1], int32([0, 0]), c.full, c.ring, 2, 31)
+    with pytest.raises(ValueError):
+        aoh_kv_append_q8(k, k, [0, 1], int32([0]), c.full, c.ring, 2, 30)
+    with pytest.raises(ValueError):
+        aoh_kv_append_q8(k, k, [0, 1], torch.zeros(2, dtype=torch.int32), c.full, c.ring, 2, 30)
+    with pytest.raises(ValueError):
+        aoh_kv_append_q8(k.cpu(), k, [0, 1], int32([0, 0]), c.full, c.ring, 2, 30)
+    torch.cuda.synchronize()
+    c.check()
