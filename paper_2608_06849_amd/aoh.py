@@ -514,14 +514,21 @@ def _q8_labels(head_is_streaming, n):
 def _q8_run(call, device, stream, *args):
     """Calls with the device's current stream (or the given one) and that device current."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        handle = _current_stream(device.index)
     elif stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the caches on {device}")
+    else:
+        handle = stream.cuda_stream
     if torch.cuda.current_device() == device.index:
-        _check(call(*args, stream.cuda_stream))
+        _check(call(*args, handle))
     else:
         with torch.cuda.device(device):
-            _check(call(*args, stream.cuda_stream))
+            _check(call(*args, handle))
+
+
+# Handle of a device's current stream: torch's own call for it, or (1.6 us slower a call) through a stream object.
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def aoh_kv_append_q8(k_new, v_new, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, stream=None):

@@ -93,13 +93,22 @@ size_t decode_need(int64_t batch, int64_t hq, int64_t d) {
   return std::max(ws_bytes(kWsMaxWgs * gs + few * hq, 2 * few * hq, d), ws_bytes(2 * kWsMaxWgs * gs, 4 * kWsMaxWgs, d));
 }
 
-// Whether a step is split by the pass for many items (decode_split.h).
+// Whether a step is split by the pass for many items (decode_split.h), which
+// starts later (its tables) but holds whole items, so it saves partials at every
+// item.  us a step, many / work-space pass, half of the heads streaming, window 512.
+// Width 128, 128 items: of four heads 27 / 30 (300-6000 tokens), 63 / 66
+// (2000-30000), of one 26 / 25, 62 / 63, of seven 28 / 34; 64 items of four 22 / 20.
+// Width 64, 128 items of four 20 / 20, 41 / 39, of one 20 / 18, 40 / 37; 256 of four
+// 26 / 30, 63 / 66, of one 26 / 26, 62 / 62, 512 of one 38 / 44.
+// In caches of 32 blocks and fewer no item is in many workgroups, which the pass for
+// many items would merge one after the other (200-500 tokens): width 128, 32 items of
+// seven heads 12.5 / 13.5, of four 12.0 / 12.1, 64 of one 12.7 / 12.5; width 64, 128
+// of four 11.9 / 13.2, 64 of four 11.6 / 10.6, 128 of one 11.8 / 11.3.
 bool takes_many(int64_t B, int64_t Hkv, int gs, int D, int64_t blocks) {
   if (B > kWsMaxBatch) return true;
-  const int64_t items = B * Hkv;
   int64_t many = D == 128 ? 128 : 256;
-  if (blocks > 32) many = D == 128 ? (gs == 1 ? 384 : gs < 4 ? 192 : 128) : (gs == 1 ? 512 : gs < 4 ? 384 : 256);
-  return items >= many;
+  if (blocks <= 32 && gs >= 4) many = D == 128 ? 32 : 128;
+  return B * Hkv >= many;
 }
 
 aoh_status decode_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new, bool step,

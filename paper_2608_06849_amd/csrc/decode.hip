@@ -456,11 +456,12 @@ template <int D, int MODE>
 struct Bf16Body {
   static constexpr int kD = D;
   static constexpr bool kScores = MODE == 1;
-  template <bool RING>
-  static __device__ __forceinline__ void run(const DecodeArgs& a, const CacheView& cv, int b, int kvl, int len,
-                                             int blk0, int blk_lim, f32x4 (&acc)[D / 16], float& m, float& l,
-                                             void* lds) {
-    decode_split_body<D, RING, !RING && MODE == 1, MODE == 3>(a, cv, b, kvl, len, blk0, blk_lim, acc, m, l, lds);
+  static constexpr int kWaves = kSplitWaves;
+  static constexpr int kPerSimd = 2;
+  static __device__ __forceinline__ void run(const DecodeArgs& a, bool ring, int b, int kvl, int len, int blk0,
+                                             int blk_lim, f32x4 (&acc)[D / 16], float& m, float& l, void* lds) {
+    if (ring) decode_split_body<D, true, false, MODE == 3>(a, a.ring, b, kvl, len, blk0, blk_lim, acc, m, l);
+    else decode_split_body<D, false, MODE == 1, MODE == 3>(a, a.full, b, kvl, len, blk0, blk_lim, acc, m, l, lds);
   }
   static __device__ __forceinline__ int dim(int t, int G) { return 16 * t + 4 * G; }
 };

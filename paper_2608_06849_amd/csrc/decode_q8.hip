@@ -18,6 +18,7 @@
 //   All addresses of a load are one uniform base and a constant offset of
 // the lane.  Block table entries are loaded 64 at a time, one a lane.
 #include <cfloat>
+#include <type_traits>
 
 #include "aoh_internal.h"
 #include "decode_split.h"
@@ -27,11 +28,11 @@ namespace aoh {
 
 namespace {
 
-constexpr int kBlocks = 4;  // blocks a wave folds at a time
 
-// Codes and scales of kBlocks blocks.
-template <int D>
+// Codes and scales of the blocks that a wave folds at a time, 16 KB.
+template <int D, int BLOCKS>
 struct Q8Chunk {
+  static constexpr int kBlocks = BLOCKS;
   u32x4 k[kBlocks][D / 64];
   u32x4 v[kBlocks][D / 64];
   u32x2 s[kBlocks];
@@ -71,16 +72,17 @@ __device__ __forceinline__ void store_token(const DecodeArgs& a, uint8_t* uk, ui
 
 }  // namespace
 
-template <int D, bool I8>
+template <int D, bool I8, int WAVES, int BLOCKS, int PER_SIMD>
 struct Q8Body {
   static constexpr int kD = D;
   static constexpr bool kScores = false;
+  static constexpr int kWaves = WAVES;
+  static constexpr int kPerSimd = PER_SIMD;
+  static constexpr int kBlocks = BLOCKS;
   static __device__ __forceinline__ int dim(int t, int G) { return 64 * (t >> 2) + 16 * G + 4 * (t & 3); }
 
-  // Scores of the blocks c .. c + kBlocks - 1 of a cache row (rows from `left` on,
-  // counted from the lane group's first one, get -inf) and V's scales.
-  static __device__ __forceinline__ void scores(const DecodeArgs& a, const Q8Chunk<D>& x, const bf16x8 (&q)[D / 32],
-                                                bool partial, int left, float (&s)[kBlocks][4], float (&vs)[kBlocks][4]) {
+  // q . k of the blocks of a chunk, unscaled by 1 / sqrt(D).
+  static __device__ __forceinline__ void scores(const Q8Chunk<D, BLOCKS>& x, const bf16x8 (&q)[D / 32], float (&s)[kBlocks][4]) {
 #pragma unroll
     for (int X = 0; X < kBlocks; ++X) {
       f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -89,100 +91,132 @@ struct Q8Body {
         sc = mfma16(codes_operand<I8>(x.k[X][i][0], x.k[X][i][1]), q[2 * i], sc);
         sc = mfma16(codes_operand<I8>(x.k[X][i][2], x.k[X][i][3]), q[2 * i + 1], sc);
       }
-      const float ks[4] = {scale_of<0>(x.s[X][0]), scale_of<16>(x.s[X][0]), scale_of<0>(x.s[X][1]), scale_of<16>(x.s[X][1])};
-      vs[X][0] = scale_of<8>(x.s[X][0]);
-      vs[X][1] = scale_of<24>(x.s[X][0]);
-      vs[X][2] = scale_of<8>(x.s[X][1]);
-      vs[X][3] = scale_of<24>(x.s[X][1]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[X][i] = sc[i] * ks[i] * a.scale_log2;
-        if (partial && 16 * X + i >= left) {
-          // rows past the end may hold anything: weight 0, and no factor that is not finite
-          s[X][i] = -INFINITY;
-          vs[X][i] = 0.f;
-        }
-      }
+      s[X][0] = sc[0] * scale_of<0>(x.s[X][0]);
+      s[X][1] = sc[1] * scale_of<2>(x.s[X][0]);
+      s[X][2] = sc[2] * scale_of<0>(x.s[X][1]);
+      s[X][3] = sc[3] * scale_of<2>(x.s[X][1]);
     }
   }
 
-  // Folds scores and V codes of kBlocks blocks into the running softmax state.
-  static __device__ __forceinline__ void fold(const DecodeArgs& a, Q8Chunk<D>& x, float (&s)[kBlocks][4],
-                                              const float (&vs)[kBlocks][4], bool partial, int left,
+  // Folds scores, V codes and V scales of a chunk into the running softmax state
+  // (m_run in units of q . k).  `left`: rows from the lane group's first one to
+  // the end, where `partial`.
+  static __device__ __forceinline__ void fold(const DecodeArgs& a, Q8Chunk<D, BLOCKS>& x, float (&s)[kBlocks][4],
+                                              const u32x2 (&vs)[kBlocks], bool partial, int left,
                                               f32x4 (&acc)[D / 16], float& m_run, float& l_run) {
-    float mx = s[0][0];
+    float w[kBlocks][4];
 #pragma unroll
-    for (int e = 1; e < 4 * kBlocks; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
-    mx = wave_xor_max(mx, 16);
-    mx = xor32_max(mx);
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = fast_exp2(m_run - m_new);
-    m_run = m_new;
-    float psum = 0.f;
-    bf16x8 w[kBlocks / 2], r[kBlocks / 2];
-#pragma unroll
-    for (int X = 0; X < kBlocks; ++X)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = fast_exp2(s[X][i] - m_new);
-        psum += p;
-        const float pv = p * vs[X][i];
-        const bf16 h = f32_to_bf16(pv);
-        w[X / 2][4 * (X & 1) + i] = h;
-        r[X / 2][4 * (X & 1) + i] = f32_to_bf16(pv - (float)h);
-      }
-    l_run = l_run * alpha + psum;
+    for (int X = 0; X < kBlocks; ++X) {
+      w[X][0] = scale_of<1>(vs[X][0]);
+      w[X][1] = scale_of<3>(vs[X][0]);
+      w[X][2] = scale_of<1>(vs[X][1]);
+      w[X][3] = scale_of<3>(vs[X][1]);
+    }
     if (partial) {
+      // Rows past the end may hold anything: score -inf, no V scale, no V code (it may be NaN).
 #pragma unroll
       for (int X = 0; X < kBlocks; ++X) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool off = 16 * X + i >= left;
+          s[X][i] = off ? -INFINITY : s[X][i];
+          w[X][i] = off ? 0.f : w[X][i];
+        }
         const int n = min(max(left - 16 * X, 0), 4);
-        const uint32_t keep = n == 4 ? ~0u : (1u << (8 * n)) - 1u;  // codes past the end may be NaN
+        const uint32_t keep = n == 4 ? ~0u : (1u << (8 * n)) - 1u;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) x.v[X][j][e] &= keep;
       }
     }
+    float mx = s[0][0];
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t)
+    for (int e = 1; e < 4 * kBlocks; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
+    mx = wave_xor_max(mx, 16);
+    mx = xor32_max(mx);
+    if (__ballot(mx > m_run)) {  // in some head; rare after the first chunks
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = fast_exp2((m_run - m_new) * a.scale_log2);
+      m_run = m_new;
+      l_run *= alpha;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
-    // acc += V^T . (w + what rounding left of the weights)^T
+      for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t)
+        for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
+    }
+    const float m_log2 = m_run * a.scale_log2;
+    float psum = 0.f;
+    u32x4 hi[kBlocks / 2];
 #pragma unroll
-      for (int P = 0; P < kBlocks / 2; ++P) {
-        const bf16x8 v = codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]);
-        acc[t] = mfma16(v, w[P], acc[t]);
-        acc[t] = mfma16(v, r[P], acc[t]);
+    for (int X = 0; X < kBlocks; ++X)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = fast_exp2(__builtin_fmaf(s[X][i], a.scale_log2, -m_log2));
+        psum += p;
+        w[X][i] *= p;
+        if (i & 1) hi[X / 2][2 * (X & 1) + i / 2] = pack_bf16(w[X][i - 1], w[X][i]);
       }
+    l_run += psum;
+    add(x, hi, acc);
+    if (a.out_f32) {
+      // The rounding errors of the weights, as a second product.  V's codes are
+      // converted again: kept from the first one they would not fit the registers.
+#pragma unroll
+      for (int X = 0; X < kBlocks; ++X) {
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) asm volatile("" : "+v"(x.v[X][j]));
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const uint32_t h = hi[X / 2][2 * (X & 1) + i / 2];
+          hi[X / 2][2 * (X & 1) + i / 2] = pack_bf16(w[X][i] - __builtin_bit_cast(float, h << 16),
+                                                     w[X][i + 1] - __builtin_bit_cast(float, h & 0xffff0000u));
+        }
+      }
+      add(x, hi, acc);
+    }
   }
 
-  template <bool RING>
-  static __device__ __forceinline__ void run(const DecodeArgs& a, const CacheView& cv, int b, int kvl, int len,
-                                             int blk0, int blk_lim, f32x4 (&out)[D / 16], float& m_out, float& l_out,
-                                             void*) {
+  // acc += V^T . W^T for the weights of a chunk's block pairs.
+  static __device__ __forceinline__ void add(const Q8Chunk<D, BLOCKS>& x, const u32x4 (&w)[kBlocks / 2], f32x4 (&acc)[D / 16]) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+#pragma unroll
+      for (int P = 0; P < kBlocks / 2; ++P)
+        acc[t] = mfma16(codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]),
+                        __builtin_bit_cast(bf16x8, w[P]), acc[t]);
+    }
+  }
+
+  static __device__ __forceinline__ void run(const DecodeArgs& a, bool ring, int b, int kvl, int len, int blk0,
+                                             int blk_lim, f32x4 (&acc)[D / 16], float& m_out, float& l_out, void*) {
+    const CacheView& cv = ring ? a.ring : a.full;
     const int lane = threadIdx.x & (kWave - 1);
     const int col = lane & 15, G = lane >> 4;
     const int g = cv.kv_heads[kvl];
     // Lengths beyond the cache capacity are clamped so no read leaves the cache.
-    const int n_valid = RING ? min(len, a.ring_cap) : min(len, cv.max_pages * kPage);
+    const int n_valid = min(len, ring ? a.ring_cap : cv.max_pages * kPage);
     const int blk_end = min(blk_lim, (n_valid + kPage - 1) / kPage);
     if (blk0 >= blk_end) return;
     const int tok_end = min(n_valid, blk_end * kPage);
 
-    // Block table entries of the 64 blocks from `first` on, one a lane.
-    const int32_t* bt = RING ? nullptr : cv.block_table + (int64_t)b * cv.max_pages;
-    auto entries = [&](int first) -> int { return RING ? 0 : bt[min(first + lane, blk_end - 1)]; };
-    const int64_t ring0 = RING ? ((int64_t)b * cv.n_kv + kvl) * cv.ring_blocks : 0;
-    // An invalid entry reads page 0, never outside the cache.
-    auto unit_of = [&](int blk, int first, int ent) -> int64_t {
-      if (RING) return ring0 + blk;
-      const int e = __builtin_amdgcn_readlane(ent, blk - first);
-      return (int64_t)((e < 0 || e >= cv.num_pages) ? 0 : e) * cv.n_kv + kvl;
+    // Unit of a block: unit0 + entry * step, with the page as the entry (an invalid
+    // one reads page 0, never outside the cache) or the ring's block.  Entries of the
+    // 64 blocks from `first` on, one a lane.
+    const int64_t unit0 = ring ? ((int64_t)b * cv.n_kv + kvl) * cv.ring_blocks : kvl;
+    const int step = ring ? 1 : cv.n_kv;
+    const int32_t* bt = cv.block_table + (int64_t)b * cv.max_pages;
+    auto entries = [&](int from) -> int {
+      const int blk = min(from + lane, blk_end - 1);
+      if (ring) return blk;
+      const int page = bt[blk];
+      return page < 0 || page >= cv.num_pages ? 0 : page;
     };
     int first = blk0;
     int ent = entries(first);
+    auto unit_of = [&](int blk) -> int64_t {
+      return unit0 + (int64_t)__builtin_amdgcn_readlane(ent, blk - first) * step;
+    };
 
     // Q^T operand: column = query head, dimensions in the order of the K loads.
     bf16x8 q[D / 32];
@@ -204,15 +238,13 @@ struct Q8Body {
       // Fused step: the wave whose range holds the token's block stores it before
       // it reads the block; no other wave reads this unit.
       const int p = len - 1;
-      const int slot = RING ? (p < a.n_sink ? p : a.n_sink + (p - a.n_sink) % a.window) : p;
+      const int slot = !ring || p < a.n_sink ? p : a.n_sink + (p - a.n_sink) % a.window;
       const int blk = slot / kPage;
       if (blk >= blk0 && blk < blk_end) {
-        int64_t unit = -1;
-        if (RING) {
-          unit = ring0 + blk;
-        } else {
+        int64_t unit = unit0 + blk;
+        if (!ring) {
           const int page = __builtin_amdgcn_readfirstlane(bt[blk]);
-          if (page >= 0 && page < cv.num_pages) unit = (int64_t)page * cv.n_kv + kvl;
+          unit = page >= 0 && page < cv.num_pages ? unit0 + (int64_t)page * step : -1;
         }
         if (unit >= 0) {
           store_token<D, I8>(a, const_cast<uint8_t*>(ck) + unit * (kPage * D), const_cast<uint8_t*>(cvv) + unit * (kPage * D),
@@ -228,12 +260,12 @@ struct Q8Body {
     // Blocks c .. c + kBlocks - 1; what lies past the end stays as it is (masked).
     // K and V of a chunk are loaded into the registers of the chunk before it, each
     // as soon as those are used up.
-    Q8Chunk<D> x;
+    Q8Chunk<D, BLOCKS> x;
     auto load_k = [&](int c) {
 #pragma unroll
       for (int X = 0; X < kBlocks; ++X) {
         if (c + X >= blk_end) break;
-        const int64_t u = unit_of(c + X, first, ent);
+        const int64_t u = unit_of(c + X);
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) x.k[X][i] = ld16_stream(ck + u * (kPage * D) + k_off + 64 * i);
         x.s[X] = ld8(cv.scales + u * kScaleBytes + 8 * G);
@@ -243,7 +275,7 @@ struct Q8Body {
 #pragma unroll
       for (int X = 0; X < kBlocks; ++X) {
         if (c + X >= blk_end) break;
-        const int64_t u = unit_of(c + X, first, ent);
+        const int64_t u = unit_of(c + X);
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) x.v[X][i] = ld16_stream(cvv + u * (kPage * D) + v_off + 1024 * i);
       }
@@ -255,9 +287,6 @@ struct Q8Body {
       x.s[X] = u32x2{0u, 0u};
     }
 
-    f32x4 acc[D / 16];
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     // Finite, so that tokens whose score is -inf have weight 0 however the range is cut.
     float m_run = -FLT_MAX, l_run = 0.f;
 
@@ -266,11 +295,14 @@ struct Q8Body {
     for (int c = blk0; c < blk_end; c += kBlocks) {
       const bool partial = (c + kBlocks) * kPage > tok_end;
       const int left = tok_end - c * kPage - 4 * G;
-      float s[kBlocks][4], vs[kBlocks][4];
-      scores(a, x, q, partial, left, s, vs);
+      float s[kBlocks][4];
+      scores(x, q, s);
+      u32x2 vs[kBlocks];
+#pragma unroll
+      for (int X = 0; X < kBlocks; ++X) vs[X] = x.s[X];
       const int next = c + kBlocks;
       if (next < blk_end) {
-        if (!RING && next + kBlocks > first + kWave) {  // entries of 64 - kBlocks blocks and more were used
+        if (next + kBlocks > first + kWave) {  // entries of 64 - kBlocks blocks and more were used
           first = next;
           ent = entries(first);
         }
@@ -280,36 +312,52 @@ struct Q8Body {
       if (next < blk_end) load_v(next);
     }
 
-    // acc[4j + n][i]: dimension 64 j + 16 G + 4 i + n
+    // acc[4j + n][i] is dimension 64 j + 16 G + 4 i + n
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t)
+    for (int j = 0; j < D / 64; ++j)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) out[t][n] = acc[(t & ~3) + n][t & 3];
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const float t = acc[4 * j + n][i];
+          acc[4 * j + n][i] = acc[4 * j + i][n];
+          acc[4 * j + i][n] = t;
+        }
     float l_tot = wave_xor_sum(l_run, 16);
     l_tot = xor32_sum(l_tot);
-    m_out = m_run;
+    m_out = m_run * a.scale_log2;
     l_out = l_tot;
   }
 };
 
 namespace {
 
-template <class Body>
+// Waves of a workgroup, blocks of a chunk and waves of a SIMD (registers).  Width
+// 128: 16 KB a chunk in 250 registers.  Width 64, work-space pass: twelve
+// waves a CU with chunks of 4 KB (16 x 131072 tokens, 4 of 8 heads streaming, e4m3: 201 us; 219
+// with eight waves and 8 KB, 217 with sixteen and 4 KB, 236 with eight and 4 KB); the
+// pass for many items gains nothing from more waves, which share items out
+// further (300 sequences of up to 900: 70 us, 104).
+template <int D, bool I8>
 void launch_body(const DecodeArgs& a, hipStream_t s) {
-  const dim3 blk(kSplitWaves * kWave);
-  if (a.many_wgs) hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), blk, 0, s, a);
-  else hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), blk, 0, s, a);
+  if (a.many_wgs) {
+    using Body = Q8Body<D, I8, 4, 4, 2>;
+    hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), dim3(Body::kWaves * kWave), 0, s, a);
+  } else {
+    using Body = std::conditional_t<D == 64, Q8Body<D, I8, 6, 2, 4>, Q8Body<D, I8, 4, 4, 2>>;
+    hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), dim3(Body::kWaves * kWave), 0, s, a);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_decode_q8_split(const DecodeArgs& a, int d, int format, hipStream_t s) {
   if (d == 64) {
-    if (format == kFormatI8) launch_body<Q8Body<64, true>>(a, s);
-    else launch_body<Q8Body<64, false>>(a, s);
+    if (format == kFormatI8) launch_body<64, true>(a, s);
+    else launch_body<64, false>(a, s);
   } else {
-    if (format == kFormatI8) launch_body<Q8Body<128, true>>(a, s);
-    else launch_body<Q8Body<128, false>>(a, s);
+    if (format == kFormatI8) launch_body<128, true>(a, s);
+    else launch_body<128, false>(a, s);
   }
   return hipGetLastError();
 }

@@ -5,10 +5,12 @@
 // both caches into ranges, has Body fold each wave's range into a softmax state,
 // and joins the states.  Body gives
 //   kD, kScores                      width; whether scores are kept (anchor layer)
-//   run<RING>(a, cv, b, kvl, len, blk0, blk_lim, acc, m, l, lds)
-//     blocks [blk0, blk_lim) of the cache row of (sequence b, KV head kvl): the
-//     unnormalised sums acc, the maximum m in log2 units and the sum l (left as
-//     they are when the range holds no token)
+//   kWaves, kPerSimd                 waves of a workgroup, and of a SIMD
+//   run(a, ring, b, kvl, len, blk0, blk_lim, acc, m, l, lds)
+//     blocks [blk0, blk_lim) of the ring or paged cache row of (sequence b, KV head
+//     kvl): the unnormalised sums acc (0 before), the maximum m in log2 units and
+//     the sum l (left as they are when the range holds no token); lds: where the
+//     wave's score codes pass (paged rows)
 //   dim(t, G)                        first of the four consecutive output
 //     dimensions that acc[t] holds in lane group G = lane / 16 (query head
 //     lane % 16 of the group)
@@ -18,7 +20,20 @@
 
 namespace aoh {
 
-// The kSplitWaves waves' partial states (acc, m in log2 units, l) merged in
+// Four output dimensions d .. d + 3 of query head hq.
+__device__ __forceinline__ void store_out4(const DecodeArgs& a, int b, int hq, int d, f32x4 o) {
+  const int64_t at = (int64_t)b * a.o_sb + (int64_t)hq * a.o_sh + d;
+  if (a.out_f32) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = o;
+  } else {
+    u32x2 w;
+    w[0] = (uint32_t)f32_to_bf16_bits(o[0]) | ((uint32_t)f32_to_bf16_bits(o[1]) << 16);
+    w[1] = (uint32_t)f32_to_bf16_bits(o[2]) | ((uint32_t)f32_to_bf16_bits(o[3]) << 16);
+    *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = w;
+  }
+}
+
+// The waves' partial states (acc, m in log2 units, l) merged in
 // LDS with log-sum-exp weights; lane (col, G) holds query head col of the
 // group, and each wave writes a share of the dimension blocks of the merged
 // partial to row `row` of part_acc / part_ml (lanes with lane_ok).  A wave
@@ -31,7 +46,8 @@ __device__ __forceinline__ void merge_waves_store(const DecodeArgs& a, f32x4 (&a
                                                   float (*s_l)[kWave], bool lane_ok, int64_t row) {
   constexpr int D = Body::kD;
   constexpr int kDimBlocks = D / 16;
-  static_assert(kDimBlocks % kSplitWaves == 0, "dimension blocks split evenly over the waves");
+  constexpr int kWaves = Body::kWaves;
+  constexpr int kPer = (kDimBlocks + kWaves - 1) / kWaves;  // dimension blocks of a wave
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & (kWave - 1);
   __syncthreads();
@@ -42,11 +58,11 @@ __device__ __forceinline__ void merge_waves_store(const DecodeArgs& a, f32x4 (&a
   __syncthreads();
   float M = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kSplitWaves; ++w) M = fmaxf(M, s_m[w][lane]);
-  float wt[kSplitWaves];
+  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][lane]);
+  float wt[kWaves];
   float L = 0.f;
 #pragma unroll
-  for (int w = 0; w < kSplitWaves; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     const float mw = s_m[w][lane];
     wt[w] = (mw == -INFINITY) ? 0.f : fast_exp2(mw - M);
     L += wt[w] * s_l[w][lane];
@@ -55,11 +71,12 @@ __device__ __forceinline__ void merge_waves_store(const DecodeArgs& a, f32x4 (&a
     const int G = lane >> 4;
     float* pa = a.part_acc + row * D;
 #pragma unroll
-    for (int k = 0; k < kDimBlocks / kSplitWaves; ++k) {
-      const int nb = wave * (kDimBlocks / kSplitWaves) + k;
+    for (int k = 0; k < kPer; ++k) {
+      const int nb = wave * kPer + k;
+      if (kPer * kWaves > kDimBlocks && nb >= kDimBlocks) break;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kSplitWaves; ++w) {
+      for (int w = 0; w < kWaves; ++w) {
         const f32x4 x = s_acc[w][nb][lane];
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] += wt[w] * x[i];
@@ -81,7 +98,7 @@ __device__ __forceinline__ void merge_waves_store(const DecodeArgs& a, f32x4 (&a
 // KV head) laid end to end, paged items first, each type in (sequence, KV
 // head) order, so one plan covers any mix of lengths and of the two cache
 // types.  Each workgroup takes one contiguous range of it and each of its
-// waves a consecutive quarter of every item segment in that range; the waves'
+// waves a consecutive share of every item segment in that range; the waves'
 // states are merged in LDS and the workgroup writes one partial per segment.
 // The launch has two workgroups per CU: the first n_cu are placed one per CU,
 // and a CU's second workgroup runs about a third slower (its waves lose issue
@@ -190,14 +207,15 @@ __device__ __forceinline__ WsItem ws_item(int g, const WsPlan& p, int B, int n_r
 }
 
 template <class Body>
-__global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_ws_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_ws_kernel(DecodeArgs a) {
   constexpr int D = Body::kD;
   constexpr int kDimBlocks = D / 16;
-  __shared__ f32x4 s_acc[kSplitWaves][kDimBlocks][kWave];
+  constexpr int kWaves = Body::kWaves;
+  __shared__ f32x4 s_acc[kWaves][kDimBlocks][kWave];
   // the score codes of each wave
-  __shared__ f32x4 s_code[Body::kScores ? kSplitWaves : 1][Body::kScores ? kDimBlocks * kWave : 1];
-  __shared__ float s_m[kSplitWaves][kWave];
-  __shared__ float s_l[kSplitWaves][kWave];
+  __shared__ f32x4 s_code[Body::kScores ? kWaves : 1][Body::kScores ? kDimBlocks * kWave : 1];
+  __shared__ float s_m[kWaves][kWave];
+  __shared__ float s_l[kWaves][kWave];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & (kWave - 1);
   int len_l, nb_l, nbr_l, P_l, Q_l;
@@ -217,18 +235,14 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_ws_kernel(Decod
     if (it.len == 0) break;
     const int s0 = g - it.off, s1 = min(g1 - it.off, it.len);
     const int len = __builtin_amdgcn_readlane(len_l, it.b);
-    // This wave's consecutive quarter of the segment's 32-token chunks.
-    const int per = ((s1 - s0 + 1) / 2 + kSplitWaves - 1) / kSplitWaves;
+    // This wave's consecutive share of the segment's 32-token chunks.
+    const int per = ((s1 - s0 + 1) / 2 + kWaves - 1) / kWaves;
     const int c0 = min(s1, s0 + 2 * per * wave), c1 = min(s1, c0 + 2 * per);
     f32x4 acc[kDimBlocks];
 #pragma unroll
     for (int nb = 0; nb < kDimBlocks; ++nb) acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    if (c0 < c1) {
-      if (it.ring) Body::template run<true>(a, a.ring, it.b, it.kvl, len, c0, c1, acc, m, l, nullptr);
-      else
-        Body::template run<false>(a, a.full, it.b, it.kvl, len, c0, c1, acc, m, l, s_code[Body::kScores ? wave : 0]);
-    }
+    if (c0 < c1) Body::run(a, it.ring, it.b, it.kvl, len, c0, c1, acc, m, l, s_code[Body::kScores ? wave : 0]);
     const int col = lane & 15;
     merge_waves_store<Body>(a, acc, m, l, s_acc, s_m, s_l, col < a.gs, (int64_t)(w + it.idx) * a.gs + col);
     if (s0 == 0 && threadIdx.x == 0) {
@@ -246,7 +260,7 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_ws_kernel(Decod
 // work space, in which every item is preceded by kItemCost places without a
 // block: what starting a segment costs a wave (its first loads), in blocks, so
 // that ranges of many short items hold fewer blocks.  Each workgroup takes one
-// contiguous range and each of its waves a consecutive quarter of it.  An item
+// contiguous range and each of its waves a consecutive share of it.  An item
 // that lies within one wave's quarter is finished and stored by that wave; the
 // pieces of an item that several waves share meet in LDS (at most two a wave:
 // the item its quarter starts in and the one it ends in), and those of several
@@ -274,16 +288,18 @@ struct ManyPlan {
 
 // Lengths and, per cache type, the exclusive prefix sums over the sequences of
 // an item's places (blocks + kItemCost; 0 for an item without blocks).
+template <int WAVES>
 struct ManyTables {
   int len[kManyMaxBatch];
   int pre[2][kManyMaxBatch + 4];
-  int carry[2][kSplitWaves];
+  int carry[2][WAVES];
 };
 
 // Fills the tables from the sequence lengths (thread t: sequences 4t .. 4t + 3)
 // and derives the plan.  Ends with a barrier.
-__device__ __forceinline__ ManyPlan many_plan(const DecodeArgs& a, ManyTables& tb) {
-  static_assert(kManyMaxBatch == 4 * kSplitWaves * kWave, "four sequences a thread");
+template <int WAVES>
+__device__ __forceinline__ ManyPlan many_plan(const DecodeArgs& a, ManyTables<WAVES>& tb) {
+  static_assert(kManyMaxBatch <= 4 * WAVES * kWave, "four sequences a thread");
   const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave;
   const bool many = a.B > 4 * kWave;  // uniform: more sequences than one wave takes
   if (wave == 0 || many) {
@@ -356,7 +372,9 @@ struct ManyItem {
   int b, kvl, off, len;
 };
 
-__device__ __forceinline__ ManyItem many_item(const DecodeArgs& a, int g, const ManyPlan& p, const ManyTables& tb) {
+template <int WAVES>
+__device__ __forceinline__ ManyItem many_item(const DecodeArgs& a, int g, const ManyPlan& p,
+                                              const ManyTables<WAVES>& tb) {
   const int lane = threadIdx.x & (kWave - 1);
   ManyItem it;
   it.ring = g >= p.paged_end;
@@ -381,19 +399,6 @@ __device__ __forceinline__ ManyItem many_item(const DecodeArgs& a, int g, const 
   return it;
 }
 
-// Four output dimensions d .. d + 3 of query head hq.
-__device__ __forceinline__ void store_out4(const DecodeArgs& a, int b, int hq, int d, f32x4 o) {
-  const int64_t at = (int64_t)b * a.o_sb + (int64_t)hq * a.o_sh + d;
-  if (a.out_f32) {
-    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = o;
-  } else {
-    u32x2 w;
-    w[0] = (uint32_t)f32_to_bf16_bits(o[0]) | ((uint32_t)f32_to_bf16_bits(o[1]) << 16);
-    w[1] = (uint32_t)f32_to_bf16_bits(o[2]) | ((uint32_t)f32_to_bf16_bits(o[3]) << 16);
-    *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = w;
-  }
-}
-
 __device__ __forceinline__ void store_ml(const DecodeArgs& a, int b, int hq, float m, float l) {
   a.ml_out[((int64_t)b * a.Hq + hq) * 2 + 0] = m;
   a.ml_out[((int64_t)b * a.Hq + hq) * 2 + 1] = l;
@@ -405,14 +410,16 @@ __device__ __forceinline__ void store_ml(const DecodeArgs& a, int b, int hq, flo
 __device__ __forceinline__ int many_slot(int first, int j) { return 2 * (first + j) + (j == 0 ? 1 : 0); }
 
 template <class Body>
-__global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_many_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_many_kernel(DecodeArgs a) {
   constexpr int D = Body::kD;
   constexpr int kDimBlocks = D / 16;
-  constexpr int kPieces = 2 * kSplitWaves;
+  constexpr int kWaves = Body::kWaves;
+  constexpr int kPieces = 2 * kWaves;
+  constexpr int kPer = (kDimBlocks + kWaves - 1) / kWaves;  // dimension blocks of a wave in the join
   __shared__ f32x4 s_acc[kPieces][kDimBlocks][kWave];
   __shared__ float s_m[kPieces][16], s_l[kPieces][16];
   __shared__ int s_g[kPieces];  // a place of the piece's segment; -1: no piece
-  __shared__ ManyTables tb;
+  __shared__ ManyTables<kWaves> tb;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & (kWave - 1);
   const int col = lane & 15, G = lane >> 4;
@@ -431,7 +438,7 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_many_kernel(Dec
   // the item shared with later workgroups that starts here: number of
   // workgroups (0: none), sequence, first query head, whether a ring
   i32x4 starts = {0, 0, 0, 0};
-  const int share = ((g1 - g0 + kSplitWaves - 1) / kSplitWaves + 1) & ~1;  // whole 32-token chunks
+  const int share = ((g1 - g0 + kWaves - 1) / kWaves + 1) & ~1;  // whole 32-token chunks
   const int e1 = min(g1, g0 + share * (wave + 1));
   for (int g = min(g1, g0 + share * wave); g < e1;) {
     const ManyItem it = many_item(a, g, p, tb);
@@ -445,9 +452,8 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_many_kernel(Dec
 #pragma unroll
     for (int nb = 0; nb < kDimBlocks; ++nb) acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    if (it.ring) Body::template run<true>(a, a.ring, it.b, it.kvl, len, s0, s1, acc, m, l, nullptr);
-    else  // the score codes pass through the wave's second piece, which only its last segment fills
-      Body::template run<false>(a, a.full, it.b, it.kvl, len, s0, s1, acc, m, l, s_acc[2 * wave + 1]);
+    // the score codes pass through the wave's second piece, which only its last segment fills
+    Body::run(a, it.ring, it.b, it.kvl, len, s0, s1, acc, m, l, s_acc[2 * wave + 1]);
     if (s0 == 0 && s1 == it.len) {  // the whole item
       const int hq = (it.ring ? a.ring : a.full).kv_heads[it.kvl] * a.gs + col;
       if (col < a.gs) {
@@ -502,17 +508,17 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_many_kernel(Dec
 #pragma unroll
     for (int q = 0; q < kPieces; ++q)
       if (g_q[q] >= at && g_q[q] < end) M = fmaxf(M, m_q[q]);
-    f32x4 o[kDimBlocks / kSplitWaves];
+    f32x4 o[kPer];
 #pragma unroll
-    for (int k = 0; k < kDimBlocks / kSplitWaves; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < kPer; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
       if (!(g_q[q] >= at && g_q[q] < end)) continue;  // uniform
       const float wt = m_q[q] == -INFINITY ? 0.f : fast_exp2(m_q[q] - M);
       L += wt * l_q[q];
 #pragma unroll
-      for (int k = 0; k < kDimBlocks / kSplitWaves; ++k) {
-        const f32x4 y = s_acc[q][wave * (kDimBlocks / kSplitWaves) + k][lane];
+      for (int k = 0; k < kPer; ++k) {
+        const f32x4 y = s_acc[q][min(wave * kPer + k, kDimBlocks - 1)][lane];
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[k][i] += wt * y[i];
       }
@@ -524,8 +530,9 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_many_kernel(Dec
       const int64_t row = (int64_t)many_slot(first, w - first) * a.gs + col;
       const float inv = 1.f / L;
 #pragma unroll
-      for (int k = 0; k < kDimBlocks / kSplitWaves; ++k) {
-        const int d = Body::dim(wave * (kDimBlocks / kSplitWaves) + k, G);
+      for (int k = 0; k < kPer; ++k) {
+        if (kPer * kWaves > kDimBlocks && wave * kPer + k >= kDimBlocks) break;
+        const int d = Body::dim(wave * kPer + k, G);
         if (ns > 1) {
           *reinterpret_cast<f32x4*>(a.part_acc + row * D + d) = o[k];
         } else {
@@ -553,7 +560,7 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void decode_many_kernel(Dec
     for (int k = 0; k < 2; ++k) {
       const CacheView& cv = k ? a.ring : a.full;
       if (!none[k]) continue;
-      for (int e = threadIdx.x; e < cv.n_kv * a.gs * (D / 4); e += kSplitWaves * kWave) {
+      for (int e = threadIdx.x; e < cv.n_kv * a.gs * (D / 4); e += kWaves * kWave) {
         const int qh = e / (D / 4), hq = cv.kv_heads[qh / a.gs] * a.gs + qh % a.gs;
         store_out4(a, b, hq, 4 * (e % (D / 4)), f32x4{a.empty, a.empty, a.empty, a.empty});
         if (Body::kScores && k == 0 && e % (D / 4) == 0) store_ml(a, b, hq, -INFINITY, 0.f);

@@ -20,11 +20,28 @@ namespace aoh {
 
 constexpr int kScaleBytes = 2 * kPage;  // of a unit
 
-// 2^(b - 127) of the scale byte in bits [shift, shift + 8) of w; infinite for 255.
-template <int SHIFT>
+// 2^(b - 127) of the scale byte b in byte BYTE of w; infinite for 255.  One
+// instruction, where the compiler shifts and masks.
+template <int BYTE>
 __device__ __forceinline__ float scale_of(uint32_t w) {
-  const uint32_t x = SHIFT <= 23 ? w << (23 - SHIFT) : w >> (SHIFT - 23);
-  return __builtin_bit_cast(float, x & 0x7f800000u);
+  static_assert(BYTE >= 0 && BYTE < 4, "byte of a word");
+  uint32_t r;
+  const uint32_t sh = 23;
+  if constexpr (BYTE == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "s"(sh), "v"(w));
+  else if constexpr (BYTE == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "s"(sh), "v"(w));
+  else if constexpr (BYTE == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "s"(sh), "v"(w));
+  else
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "s"(sh), "v"(w));
+  return __builtin_bit_cast(float, r);
+}
+
+// Two floats rounded to bf16, the first in the low half.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
 // Offset of the V code of dimension d, row r in its unit.
