@@ -362,6 +362,7 @@ typedef struct {
  * (bf16 or fp32 in).  start_pos may be NULL (every sequence starts at 0).
  * Positions beyond the block table, in unmapped pages (entries outside
  * [0, num_pages)) and of sequences with start_pos < 0 or >= 2^30 are not written.
+ * AOH_ERR_UNSUPPORTED for more than 2^26 tokens a sequence (here and below).
  */
 aoh_status aoh_kv_append_q8(const aoh_tensor* k_new, const aoh_tensor* v_new, const uint8_t* head_is_streaming,
                             const int32_t* start_pos, const aoh_paged_cache_q8* kv_full,

@@ -51,7 +51,7 @@ aoh_status fill_args(const aoh_paged_cache_q8* full, const aoh_ring_cache_q8* ri
                      int n_sink, int window, int64_t B, int64_t n, int64_t Hkv, int64_t D, Q8Args* a, int* format) {
   aoh_status st;
   if (D != 64 && D != 128) return fail(AOH_ERR_UNSUPPORTED, "D=%lld; supported: 64, 128", (long long)D);
-  if (n > kMaxPos) return fail(AOH_ERR_UNSUPPORTED, "%lld tokens a sequence are too many", (long long)n);
+  if (n > kMaxTokens) return fail(AOH_ERR_UNSUPPORTED, "%lld tokens a sequence are too many", (long long)n);
   if (B > (1ll << 31) - 1) return fail(AOH_ERR_UNSUPPORTED, "batch too large");
   if ((st = check_mask_params(n_sink, window))) return st;
   HeadSchedule hs;
@@ -69,8 +69,8 @@ aoh_status fill_args(const aoh_paged_cache_q8* full, const aoh_ring_cache_q8* ri
     a->ring_blocks = (int)ceil_div(ring->capacity, kPageTokens);
   }
   a->n_sink = n_sink; a->window = window;
-  a->streaming_mask = hs.streaming_mask;
-  std::memcpy(a->rank, hs.rank, sizeof(a->rank));
+  std::memcpy(a->ret, hs.ret, hs.n_ret);
+  std::memcpy(a->str, hs.str, hs.n_str);
   return AOH_OK;
 }
 

@@ -178,9 +178,10 @@ struct AppendArgs {
   uint8_t rank[kMaxKvHeads];    // rank of each KV head inside its cache
 };
 
-// Formats of the 8-bit caches (aoh_dtype values), and the bound on positions.
+// Formats of the 8-bit caches (aoh_dtype values), and the bounds on positions and
+// on the tokens of a sequence that a call writes or reads.
 constexpr int kFormatE4m3 = 2, kFormatI8 = 3;
-constexpr int kMaxPos = 1 << 30;
+constexpr int kMaxPos = 1 << 30, kMaxTokens = 1 << 26;
 
 // Writing tokens into the 8-bit caches, or reading them back into k / v.
 struct Q8Args {
@@ -203,9 +204,12 @@ struct Q8Args {
   uint8_t* rs;
   int32_t n_str, ring_blocks;
   int32_t n_sink, window;
-  int32_t chunk0;               // first 16-position chunk of the launch
-  uint64_t streaming_mask;
-  uint8_t rank[kMaxKvHeads];
+  // Workgroups of a sequence, from x0 on: `groups` of 16-position chunks for each
+  // paged head, ring_groups for each ring: its ring_sinks pages with sinks, then
+  // those of the window (ring_sinks < 0: every chunk).
+  int32_t x0, groups, ring_groups, ring_sinks;
+  uint8_t ret[kMaxKvHeads];     // KV head ids by rank in their cache
+  uint8_t str[kMaxKvHeads];
 };
 hipError_t launch_q8(const Q8Args& a, int dtype, int format, int d, bool write, hipStream_t s);
 // Split pass of a decode step over the 8-bit caches (a.ws_cu, a.many_wgs as in launch_decode_split).

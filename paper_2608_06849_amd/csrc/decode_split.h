@@ -6,6 +6,7 @@
 // and joins the states.  Body gives
 //   kD, kScores                      width; whether scores are kept (anchor layer)
 //   kWaves, kPerSimd                 waves of a workgroup, and of a SIMD
+//   kItemCost                        what starting a segment costs a wave, in blocks
 //   run(a, ring, b, kvl, len, blk0, blk_lim, acc, m, l, lds)
 //     blocks [blk0, blk_lim) of the ring or paged cache row of (sequence b, KV head
 //     kvl): the unnormalised sums acc (0 before), the maximum m in log2 units and
@@ -276,8 +277,6 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_w
 // capacity 8192: 160 us a step here, 333 with fixed splits; 64 of 200-400
 // tokens: 28 us here, 51 with the other work-space kernel.  Bound: HBM, 5.4-6
 // TB/s for full ranges.
-constexpr int kItemCost = 4;
-
 struct ManyPlan {
   int paged_end;        // places of the paged items
   int total;            // places of all items
@@ -297,7 +296,7 @@ struct ManyTables {
 
 // Fills the tables from the sequence lengths (thread t: sequences 4t .. 4t + 3)
 // and derives the plan.  Ends with a barrier.
-template <int WAVES>
+template <int WAVES, int COST>
 __device__ __forceinline__ ManyPlan many_plan(const DecodeArgs& a, ManyTables<WAVES>& tb) {
   static_assert(kManyMaxBatch <= 4 * WAVES * kWave, "four sequences a thread");
   const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave;
@@ -311,8 +310,8 @@ __device__ __forceinline__ ManyPlan many_plan(const DecodeArgs& a, ManyTables<WA
       const int l = max(len, 0);
       const int nb = a.full.n_kv ? (min(l, a.full.max_pages * kPage) + kPage - 1) / kPage : 0;
       const int nbr = a.ring.n_kv ? (min(l, a.ring_cap) + kPage - 1) / kPage : 0;
-      n[0][u] = nb ? nb + kItemCost : 0;
-      n[1][u] = nbr ? nbr + kItemCost : 0;
+      n[0][u] = nb ? nb + COST : 0;
+      n[1][u] = nbr ? nbr + COST : 0;
       if (b < a.B) tb.len[b] = len;
 #pragma unroll
       for (int k = 0; k < 2; ++k) sum[k] += n[k][u];
@@ -372,7 +371,7 @@ struct ManyItem {
   int b, kvl, off, len;
 };
 
-template <int WAVES>
+template <int WAVES, int COST>
 __device__ __forceinline__ ManyItem many_item(const DecodeArgs& a, int g, const ManyPlan& p,
                                               const ManyTables<WAVES>& tb) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -395,7 +394,7 @@ __device__ __forceinline__ ManyItem many_item(const DecodeArgs& a, int g, const 
   const int places = max(1, __builtin_amdgcn_readfirstlane(pre[it.b + 1]) - p0);
   it.kvl = (g - base - heads * p0) / places;
   it.off = base + heads * p0 + it.kvl * places;
-  it.len = places - kItemCost;
+  it.len = places - COST;
   return it;
 }
 
@@ -414,6 +413,7 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
   constexpr int D = Body::kD;
   constexpr int kDimBlocks = D / 16;
   constexpr int kWaves = Body::kWaves;
+  constexpr int kItemCost = Body::kItemCost;
   constexpr int kPieces = 2 * kWaves;
   constexpr int kPer = (kDimBlocks + kWaves - 1) / kWaves;  // dimension blocks of a wave in the join
   __shared__ f32x4 s_acc[kPieces][kDimBlocks][kWave];
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
   const int lane = threadIdx.x & (kWave - 1);
   const int col = lane & 15, G = lane >> 4;
   if (threadIdx.x < kPieces) s_g[threadIdx.x] = -1;
-  const ManyPlan p = many_plan(a, tb);
+  const ManyPlan p = many_plan<kWaves, kItemCost>(a, tb);
   const int w = blockIdx.x;
 
   int g0, g1;
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
   const int share = ((g1 - g0 + kWaves - 1) / kWaves + 1) & ~1;  // whole 32-token chunks
   const int e1 = min(g1, g0 + share * (wave + 1));
   for (int g = min(g1, g0 + share * wave); g < e1;) {
-    const ManyItem it = many_item(a, g, p, tb);
+    const ManyItem it = many_item<kWaves, kItemCost>(a, g, p, tb);
     const int v0 = g - it.off, v1 = min(e1 - it.off, it.len + kItemCost);
     const int s0 = max(0, v0 - kItemCost), s1 = v1 - kItemCost;
     const int at = g;
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
     for (int q = kPieces - 1; q >= 0; --q)
       if (g_q[q] >= from) at = g_q[q];
     if (at == INT32_MAX) break;
-    const ManyItem it = many_item(a, at, p, tb);
+    const ManyItem it = many_item<kWaves, kItemCost>(a, at, p, tb);
     const int end = it.off + it.len + kItemCost;
     from = end;
     float M = -INFINITY, L = 0.f;

@@ -177,6 +177,23 @@ def test_packed_tokens_equal_dense_ones():
             c.check(f"max_new {max_new}, start {with_start}")
 
 
+def test_packed_tokens_of_many_sequences():
+    # so many sequences and so loose a bound that a workgroup takes two chunks
+    counts = np.random.default_rng(7).integers(0, 50, 200).tolist()
+    starts = np.random.default_rng(8).integers(0, 60, 200).tolist()
+    labels, d, n_sink, window = [0, 1], 64, 4, 28
+    assert (sum(counts) // 16 + 1) * 200 >= 32768
+    c = Caches(q8.I8, labels, d, 200, 7, n_sink, window, 18)
+    k, v = (rows((sum(counts), 2, d), 18, f"q8-loose-{s}") for s in "kv")
+    cu = np.concatenate([[0], np.cumsum(counts)])
+    aoh_kv_append_q8_varlen(k, v, int32(cu.tolist()), 1 << 20, labels, int32(starts), c.full, c.ring, n_sink, window)
+    kd, vd = (torch.zeros((200, 50, 2, d), dtype=BF, device=DEV) for _ in range(2))
+    for b, n in enumerate(counts):
+        kd[b, :n], vd[b, :n] = k[cu[b]:cu[b + 1]], v[cu[b]:cu[b + 1]]
+    c.append(kd, vd, starts, counts)
+    c.check()
+
+
 def test_packed_entries_are_clamped():
     c = Caches(q8.I8, [0], 64, 3, 4, 0, 1, 9)
     k = rows((20, 1, 64), 9, "q8-clamp")
