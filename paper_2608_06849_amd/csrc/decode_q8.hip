@@ -1,15 +1,22 @@
 // Single-token decode over the 8-bit caches (layout and codes: q8.h; ranges,
 // merging and output: decode_split.h).
 //
-// A wave takes the blocks of its range four at a time (64 tokens, 16 KB at
-// d_head 128), the next four loading while it folds these:
+// A wave folds a few blocks of its range at a time (a chunk: 64 tokens, 16 KB at
+// d_head 128), the next ones loading meanwhile:
 //   S^T[16 tokens x 16 heads] = K[16 x 32 dims] . Q^T       (D/32 steps a block)
 //   O^T[16 dims x 16 heads]  += V^T[16 dims x 32 tokens] . P^T   (D/16 a block pair)
 // with v_mfma_f32_16x16x32_bf16 on codes converted to bf16, exactly.  K's row
-// scale multiplies the scores (with log2(e) / sqrt(D)) and V's the
-// probabilities, where it is exact too: a probability is rounded to bf16, as in
-// the bf16 caches' pass, or for fp32 outputs kept as the sum of two bf16 numbers
-// (2^-17 of itself), which costs a second product.
+// scale multiplies the scores and V's the probabilities, exactly too: only the
+// weight, probability times V's scale, is rounded to bf16, as in the bf16 caches'
+// pass, or for fp32 outputs kept as the sum of two bf16 numbers (2^-16 of itself),
+// which costs a second product.
+//   Bound: HBM.  8 sequences of 131072 tokens, 4 of 8 heads streaming, e4m3: 175 us
+// in the pass (1.09 GB of codes and scales, 1.03 times that fetched), 6.2 TB/s;
+// with an exponential only for every fourth score, or without converting codes, not
+// 1% less.  Width 64, whose pieces of memory are half as long: 5.4 TB/s.  Short
+// steps: a chain of memory latencies (lengths, block table, K, the join, the merge
+// launch).  The registers decide: with two chunks in flight the width 128 body
+// spilled, and the step above took 434 us.
 //   Lane group G = lane / 16 receives the scores of rows 4G .. 4G + 3 of a block,
 // and the k index of the second product is ordered so that it needs just those: P^T
 // stays in its lanes, and the V operand of dimension block 4j + n is word n of two
@@ -28,8 +35,7 @@ namespace aoh {
 
 namespace {
 
-
-// Codes and scales of the blocks that a wave folds at a time, 16 KB.
+// Codes and scales of the blocks that a wave folds at a time.
 template <int D, int BLOCKS>
 struct Q8Chunk {
   static constexpr int kBlocks = BLOCKS;
@@ -72,7 +78,8 @@ __device__ __forceinline__ void store_token(const DecodeArgs& a, uint8_t* uk, ui
 
 }  // namespace
 
-template <int D, bool I8, int WAVES, int BLOCKS, int PER_SIMD>
+// TWO: weights as two bf16 numbers.
+template <int D, bool I8, bool TWO, int WAVES, int BLOCKS, int PER_SIMD>
 struct Q8Body {
   static constexpr int kD = D;
   static constexpr bool kScores = false;
@@ -147,47 +154,33 @@ struct Q8Body {
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
     }
-    const float m_log2 = m_run * a.scale_log2;
     float psum = 0.f;
-    u32x4 hi[kBlocks / 2];
+    u32x4 hi[kBlocks / 2], lo[kBlocks / 2];
 #pragma unroll
     for (int X = 0; X < kBlocks; ++X)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = fast_exp2(__builtin_fmaf(s[X][i], a.scale_log2, -m_log2));
+        const float p = fast_exp2((s[X][i] - m_run) * a.scale_log2);  // the maximum's is 1 at any magnitude
         psum += p;
         w[X][i] *= p;
-        if (i & 1) hi[X / 2][2 * (X & 1) + i / 2] = pack_bf16(w[X][i - 1], w[X][i]);
-      }
-    l_run += psum;
-    add(x, hi, acc);
-    if (a.out_f32) {
-      // The rounding errors of the weights, as a second product.  V's codes are
-      // converted again: kept from the first one they would not fit the registers.
-#pragma unroll
-      for (int X = 0; X < kBlocks; ++X) {
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) asm volatile("" : "+v"(x.v[X][j]));
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          const uint32_t h = hi[X / 2][2 * (X & 1) + i / 2];
-          hi[X / 2][2 * (X & 1) + i / 2] = pack_bf16(w[X][i] - __builtin_bit_cast(float, h << 16),
-                                                     w[X][i + 1] - __builtin_bit_cast(float, h & 0xffff0000u));
+        if (i & 1) {
+          const uint32_t h = pack_bf16(w[X][i - 1], w[X][i]);
+          hi[X / 2][2 * (X & 1) + i / 2] = h;
+          if constexpr (TWO)
+            lo[X / 2][2 * (X & 1) + i / 2] = pack_bf16(w[X][i - 1] - __builtin_bit_cast(float, h << 16),
+                                                       w[X][i] - __builtin_bit_cast(float, h & 0xffff0000u));
         }
       }
-      add(x, hi, acc);
-    }
-  }
-
-  // acc += V^T . W^T for the weights of a chunk's block pairs.
-  static __device__ __forceinline__ void add(const Q8Chunk<D, BLOCKS>& x, const u32x4 (&w)[kBlocks / 2], f32x4 (&acc)[D / 16]) {
+    l_run += psum;
+    // acc += V^T . W^T
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
+    for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-      for (int P = 0; P < kBlocks / 2; ++P)
-        acc[t] = mfma16(codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]),
-                        __builtin_bit_cast(bf16x8, w[P]), acc[t]);
-    }
+      for (int P = 0; P < kBlocks / 2; ++P) {
+        const bf16x8 v = codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]);
+        acc[t] = mfma16(v, __builtin_bit_cast(bf16x8, hi[P]), acc[t]);
+        if constexpr (TWO) acc[t] = mfma16(v, __builtin_bit_cast(bf16x8, lo[P]), acc[t]);
+      }
   }
 
   static __device__ __forceinline__ void run(const DecodeArgs& a, bool ring, int b, int kvl, int len, int blk0,
@@ -214,6 +207,7 @@ struct Q8Body {
       const int page = bt[blk];
       return page < 0 || page >= cv.num_pages ? 0 : page;
     };
+    static_assert(kWave % kBlocks == 0, "a chunk's entries are in one register");
     int first = blk0;
     int ent = entries(first);
     auto unit_of = [&](int blk) -> int64_t {
@@ -236,7 +230,7 @@ struct Q8Body {
 
     const uint8_t* ck = reinterpret_cast<const uint8_t*>(cv.k);
     const uint8_t* cvv = reinterpret_cast<const uint8_t*>(cv.v);
-    if (a.k_new) {
+    if (a.k_new && len <= kMaxPos) {
       // Fused step: the wave whose range holds the token's block stores it before
       // it reads the block; no other wave reads this unit.
       const int p = len - 1;
@@ -304,7 +298,7 @@ struct Q8Body {
       for (int X = 0; X < kBlocks; ++X) vs[X] = x.s[X];
       const int next = c + kBlocks;
       if (next < blk_end) {
-        if (next + kBlocks > first + kWave) {  // entries of 64 - kBlocks blocks and more were used
+        if (next == first + kWave) {
           first = next;
           ent = entries(first);
         }
@@ -335,31 +329,38 @@ struct Q8Body {
 namespace {
 
 // Waves of a workgroup, blocks of a chunk and waves of a SIMD (registers).  Width
-// 128: 16 KB a chunk in 250 registers.  Width 64, work-space pass: twelve
-// waves a CU with chunks of 4 KB (16 x 131072 tokens, 4 of 8 heads streaming, e4m3: 201 us; 219
-// with eight waves and 8 KB, 217 with sixteen and 4 KB, 236 with eight and 4 KB); the
-// pass for many items gains nothing from more waves, which share items out
-// further (300 sequences of up to 900: 70 us, 104).
-template <int D, bool I8>
+// 128: chunks of 16 KB in 250 registers, two workgroups of four waves a CU.  Width
+// 64, work-space pass: two of six waves with chunks of 4 KB (16 x 131072 tokens, 4 of
+// 8 heads streaming, e4m3: 202 us; 220 with four waves and 8 KB, 218 with eight and
+// 4 KB, 236 with four and 4 KB).  The pass for many items keeps four waves, since
+// more of them cut the items further (300 sequences of up to 900 tokens: 70 us, 104
+// with six waves).
+template <int D, bool I8, bool TWO>
 void launch_body(const DecodeArgs& a, hipStream_t s) {
   if (a.many_wgs) {
-    using Body = Q8Body<D, I8, 4, 4, 2>;
+    using Body = Q8Body<D, I8, TWO, 4, 4, 2>;
     hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), dim3(Body::kWaves * kWave), 0, s, a);
   } else {
-    using Body = std::conditional_t<D == 64, Q8Body<D, I8, 6, 2, 4>, Q8Body<D, I8, 4, 4, 2>>;
+    using Body = std::conditional_t<D == 64, Q8Body<D, I8, TWO, 6, 2, 4>, Q8Body<D, I8, TWO, 4, 4, 2>>;
     hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), dim3(Body::kWaves * kWave), 0, s, a);
   }
+}
+
+template <int D, bool I8>
+void launch_format(const DecodeArgs& a, hipStream_t s) {
+  if (a.out_f32) launch_body<D, I8, true>(a, s);
+  else launch_body<D, I8, false>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_decode_q8_split(const DecodeArgs& a, int d, int format, hipStream_t s) {
   if (d == 64) {
-    if (format == kFormatI8) launch_body<64, true>(a, s);
-    else launch_body<64, false>(a, s);
+    if (format == kFormatI8) launch_format<64, true>(a, s);
+    else launch_format<64, false>(a, s);
   } else {
-    if (format == kFormatI8) launch_body<128, true>(a, s);
-    else launch_body<128, false>(a, s);
+    if (format == kFormatI8) launch_format<128, true>(a, s);
+    else launch_format<128, false>(a, s);
   }
   return hipGetLastError();
 }
