@@ -121,7 +121,7 @@ def copy_calibration():
 # the sources its kernel is built from: a change to them makes the figure
 # stale and it is dropped.
 PREFILL_SOURCES = ("prefill.hip", "aoh_device.h", "aoh_internal.h")
-DECODE_SOURCES = ("decode.hip", "aoh_device.h", "aoh_internal.h")
+DECODE_SOURCES = ("decode.hip", "decode_split.h", "aoh_device.h", "aoh_internal.h")
 TRAFFIC = {
     "fetch_factor": 524301.2 / 1048576.0,   # FETCH_SIZE of a 1 GiB copy / 1 GiB
     "write_factor": 1048576.0 / 1048576.0,  # WRITE_SIZE of a 1 GiB copy / 1 GiB

@@ -8,8 +8,9 @@
 // with v_mfma_f32_16x16x32_bf16 on codes converted to bf16, exactly.  K's row
 // scale multiplies the scores and V's the probabilities, exactly too: only the
 // weight, probability times V's scale, is rounded to bf16, as in the bf16 caches'
-// pass, or for fp32 outputs kept as the sum of two bf16 numbers (2^-16 of itself),
-// which costs a second product.
+// pass, or for fp32 outputs kept whole as the sum of three bf16 numbers, which costs
+// two more products (16 sequences of 2000-32000 tokens, width 64: 41.3 us a step,
+// 39.6 with two numbers and 2^-18 of each weight lost; width 128: 0-1.5%).
 //   Bound: HBM.  8 sequences of 131072 tokens, 4 of 8 heads streaming, e4m3: 175 us
 // in the pass (1.09 GB of codes and scales, 1.03 times that fetched), 6.2 TB/s;
 // with an exponential only for every fourth score, or without converting codes, not
@@ -78,8 +79,8 @@ __device__ __forceinline__ void store_token(const DecodeArgs& a, uint8_t* uk, ui
 
 }  // namespace
 
-// TWO: weights as two bf16 numbers.
-template <int D, bool I8, bool TWO, int WAVES, int BLOCKS, int PER_SIMD>
+// WHOLE: weights unrounded, as the sums of three bf16 numbers.
+template <int D, bool I8, bool WHOLE, int WAVES, int BLOCKS, int PER_SIMD>
 struct Q8Body {
   static constexpr int kD = D;
   static constexpr bool kScores = false;
@@ -155,7 +156,8 @@ struct Q8Body {
         for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
     }
     float psum = 0.f;
-    u32x4 hi[kBlocks / 2], lo[kBlocks / 2];
+    constexpr int kParts = WHOLE ? 3 : 1;
+    u32x4 part[kBlocks / 2][kParts];
 #pragma unroll
     for (int X = 0; X < kBlocks; ++X)
 #pragma unroll
@@ -163,12 +165,20 @@ struct Q8Body {
         const float p = fast_exp2((s[X][i] - m_run) * a.scale_log2);  // the maximum's is 1 at any magnitude
         psum += p;
         w[X][i] *= p;
-        if (i & 1) {
-          const uint32_t h = pack_bf16(w[X][i - 1], w[X][i]);
-          hi[X / 2][2 * (X & 1) + i / 2] = h;
-          if constexpr (TWO)
-            lo[X / 2][2 * (X & 1) + i / 2] = pack_bf16(w[X][i - 1] - __builtin_bit_cast(float, h << 16),
-                                                       w[X][i] - __builtin_bit_cast(float, h & 0xffff0000u));
+        if (!(i & 1)) continue;
+        const int word = 2 * (X & 1) + i / 2;
+        if constexpr (WHOLE) {
+          // the upper eight bits, the next eight of what is left, the last eight
+          float w0 = w[X][i - 1], w1 = w[X][i];
+#pragma unroll
+          for (int n = 0; n < kParts; ++n) {
+            const uint32_t b0 = __builtin_bit_cast(uint32_t, w0), b1 = __builtin_bit_cast(uint32_t, w1);
+            part[X / 2][n][word] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            w0 -= __builtin_bit_cast(float, b0 & 0xffff0000u);
+            w1 -= __builtin_bit_cast(float, b1 & 0xffff0000u);
+          }
+        } else {
+          part[X / 2][0][word] = pack_bf16(w[X][i - 1], w[X][i]);
         }
       }
     l_run += psum;
@@ -178,8 +188,8 @@ struct Q8Body {
 #pragma unroll
       for (int P = 0; P < kBlocks / 2; ++P) {
         const bf16x8 v = codes_operand<I8>(x.v[2 * P][t >> 2][t & 3], x.v[2 * P + 1][t >> 2][t & 3]);
-        acc[t] = mfma16(v, __builtin_bit_cast(bf16x8, hi[P]), acc[t]);
-        if constexpr (TWO) acc[t] = mfma16(v, __builtin_bit_cast(bf16x8, lo[P]), acc[t]);
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) acc[t] = mfma16(v, __builtin_bit_cast(bf16x8, part[P][n]), acc[t]);
       }
   }
 
@@ -335,13 +345,13 @@ namespace {
 // 4 KB, 236 with four and 4 KB).  The pass for many items keeps four waves, since
 // more of them cut the items further (300 sequences of up to 900 tokens: 70 us, 104
 // with six waves).
-template <int D, bool I8, bool TWO>
+template <int D, bool I8, bool WHOLE>
 void launch_body(const DecodeArgs& a, hipStream_t s) {
   if (a.many_wgs) {
-    using Body = Q8Body<D, I8, TWO, 4, 4, 2>;
+    using Body = Q8Body<D, I8, WHOLE, 4, 4, 2>;
     hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), dim3(Body::kWaves * kWave), 0, s, a);
   } else {
-    using Body = std::conditional_t<D == 64, Q8Body<D, I8, TWO, 6, 2, 4>, Q8Body<D, I8, TWO, 4, 4, 2>>;
+    using Body = std::conditional_t<D == 64, Q8Body<D, I8, WHOLE, 6, 2, 4>, Q8Body<D, I8, WHOLE, 4, 4, 2>>;
     hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), dim3(Body::kWaves * kWave), 0, s, a);
   }
 }

@@ -92,7 +92,7 @@ __device__ __forceinline__ void merge_waves_store(const DecodeArgs& a, f32x4 (&a
 }
 
 // ---------------------------------------------------------------------------
-// Split pass over the step's work space (bf16 plain, anchor and fused-step
+// Split pass over the step's work space (plain, anchor and fused-step
 // decode of up to kWsMaxBatch sequences).
 //
 // Work space: the valid 16-token blocks of every item (cache type, sequence,
@@ -262,9 +262,9 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_w
 // block: what starting a segment costs a wave (its first loads), in blocks, so
 // that ranges of many short items hold fewer blocks.  Each workgroup takes one
 // contiguous range and each of its waves a consecutive share of it.  An item
-// that lies within one wave's quarter is finished and stored by that wave; the
+// that lies within one wave's share is finished and stored by that wave; the
 // pieces of an item that several waves share meet in LDS (at most two a wave:
-// the item its quarter starts in and the one it ends in), and those of several
+// the item its share starts in and the one it ends in), and those of several
 // workgroups in the workspace, for the merge launch, which finds them through
 // ws_items: by workgroup, the item that starts in it and goes on, if any.
 //
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
         if (Body::kScores && !it.ring && G == 0) store_ml(a, it.b, hq, m, l);
       }
     } else {
-      // the wave's last segment unless the item began before its quarter
+      // the wave's last segment unless the item began before its share
       const int piece = 2 * wave + (s0 == 0 ? 1 : 0);
 #pragma unroll
       for (int nb = 0; nb < kDimBlocks; ++nb) s_acc[piece][nb][lane] = acc[nb];

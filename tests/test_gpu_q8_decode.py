@@ -6,9 +6,9 @@ Bound of an output element, with A = sum_j w_j |v_j| (w the exact weights), T ke
     ds = (D + 4) 2^-24 max_j sum_d |q_d k_jd| / sqrt(D); so a weight by a factor exp(2 ds) at most (its own score and
     the sum's), plus 2^-21 for the exponentials, whose arguments in log2 units are rounded once more;
   weights: to bf16 for a bf16 output, half a step of which is 2^-8 of the weight (torch.finfo(torch.bfloat16).eps / 2);
-    for an fp32 output as two bf16 numbers, the second of what the first left: 2^-8 of 2^-8, so 2^-16;
+    for an fp32 output as three bf16 numbers of 8 significant bits each, which hold fp32's 24;
   sums over T keys in fp32, joined over at most 512 partials: (T + 512 + 16) 2^-24 of the absolute sum, for numerator
-    and denominator;
+    and denominator (the three parts of a weight are three terms of the numerator);
   the output's rounding: 2^-8 of the value (bf16) or 2^-24 (fp32).
 """
 import numpy as np
@@ -88,8 +88,8 @@ class Run:
         big = np.abs(q).reshape(len(on), len(self.labels), -1, self.d)
         s = np.einsum("bhgd,bthd->bhgt", big, np.abs(self.ks[on][:, :top])).max(-1) / np.sqrt(self.d)
         ds = (self.d + 4) * 2.0 ** -24 * s.reshape(len(on), -1, 1)
-        weight = 2.0 ** (-8 if got.dtype == BF else -16)
-        rel = np.expm1(2 * ds) + 2.0 ** -21 + weight + 2 * (top + 528) * 2.0 ** -24
+        weight, parts = (2.0 ** -8, 1) if got.dtype == BF else (0.0, 3)
+        rel = np.expm1(2 * ds) + 2.0 ** -21 + weight + ((1 + parts) * top + 2 * 528) * 2.0 ** -24
         step = 2.0 ** -8 if got.dtype == BF else 2.0 ** -24
         err = np.abs(g[on] - want)
         bound = rel * spread + step * (np.abs(want) + rel * spread)
