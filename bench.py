@@ -123,12 +123,12 @@ def copy_calibration():
 PREFILL_SOURCES = ("prefill.hip", "aoh_device.h", "aoh_internal.h")
 DECODE_SOURCES = ("decode.hip", "decode_split.h", "aoh_device.h", "aoh_internal.h")
 TRAFFIC = {
-    "fetch_factor": 524301.2 / 1048576.0,   # FETCH_SIZE of a 1 GiB copy / 1 GiB
+    "fetch_factor": 524299.7 / 1048576.0,   # FETCH_SIZE of a 1 GiB copy / 1 GiB
     "write_factor": 1048576.0 / 1048576.0,  # WRITE_SIZE of a 1 GiB copy / 1 GiB
-    "prefill_mixed": {"fetch_kib": 462558.9, "write_kib": 263395.6,
-                      "sources": PREFILL_SOURCES, "source_hash": "df215c67e08a47a0"},
-    "decode_ws": {"fetch_kib": 1081406.2, "write_kib": 1169.9,
-                  "sources": DECODE_SOURCES, "source_hash": "97176a0d44d1761e"},
+    "prefill_mixed": {"fetch_kib": 465775.0, "write_kib": 263396.3,
+                      "sources": PREFILL_SOURCES, "source_hash": "f5ebfbb1542746d2"},
+    "decode_ws": {"fetch_kib": 1081132.8, "write_kib": 1169.8,
+                  "sources": DECODE_SOURCES, "source_hash": "d27c6acbc989ac47"},
 }
 
 

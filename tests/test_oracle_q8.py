@@ -57,6 +57,17 @@ def test_rows_without_a_scale(fmt):
     assert np.isnan(q8.values(codes, scales, fmt)[1:4]).all() and not q8.values(codes, scales, fmt)[4].any()
 
 
+@pytest.mark.parametrize("fmt", [q8.E4M3, q8.I8])
+def test_stored_values_are_stored_as_themselves(fmt):
+    rng = np.random.default_rng(4)
+    x = rng.standard_normal((300, 64)) * np.exp2(rng.integers(-140, 120, (300, 1)))
+    # a maximum that rounds down to half of the largest code: the next scale below holds it as well
+    x[:40] = rng.standard_normal((40, 64)) * 8
+    x[:40, 0] = q8.largest(fmt) / 2 * (1 + 2.0 ** -6)
+    once = q8.stored(x, fmt)
+    assert np.array_equal(q8.stored(once, fmt), once)
+
+
 def test_v_layout_round_trip():
     rows = np.arange(2 * 16 * 64).reshape(2, 16, 64)
     unit = q8.v_unit(rows)
