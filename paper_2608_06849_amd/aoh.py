@@ -271,11 +271,21 @@ class RingCache:
         return c
 
 
-class PagedCacheQ8:
+class _Fixed:
+    """Attributes are set once: a descriptor made from them stays true."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__:
+            raise AttributeError(f"{name} of a {type(self).__name__} cannot be replaced; make another one")
+        super().__setattr__(name, value)
+
+
+class PagedCacheQ8(_Fixed):
     """Retrieval-head cache in 8 bits (torch.float8_e4m3fn or torch.int8): K codes [pages, heads, 16, D], V codes
     [pages, heads, D/4, 4, 4, 4] (dim // 4, row // 4, dim % 4, row % 4), scale bytes [pages, heads, 16, 2] (K, V;
     uint8), and a per-sequence block table (int32), all contiguous and on one device.  The object keeps the
-    descriptor that the calls pass on, so its tensors stay the same."""
+    descriptor that the calls pass on, so its tensors cannot be replaced (`rows` or another object over the same
+    tensors takes another table)."""
 
     def __init__(self, k, v, scales, block_table):
         pages, heads, _, d = k.shape
@@ -298,7 +308,7 @@ class PagedCacheQ8:
         return PagedCacheQ8(self.k, self.v, self.scales, self.block_table[b0:b1])
 
 
-class RingCacheQ8:
+class RingCacheQ8(_Fixed):
     """Streaming-head cache in 8 bits: n_sink + window slots per (sequence, head), padded to whole 16-slot blocks,
     each laid out as a page of PagedCacheQ8: K codes [batch, heads, blocks, 16, D] and so on."""
 

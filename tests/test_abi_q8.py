@@ -220,3 +220,13 @@ def test_binding_refuses_host_tensors_and_mismatches():
         A._q8_seqs(lens, "lens", torch.device("cpu"), 3)
     with pytest.raises(ValueError, match="labels"):
         A._q8_labels([0, 1], 3)
+
+
+def test_cache_tensors_cannot_be_replaced():
+    # the calls pass on the descriptor made with the object: another table or pool would not be seen
+    full = A.PagedCacheQ8.allocate(3, 2, 64, torch.int8, torch.zeros(2, 2, dtype=torch.int32), device="cpu")
+    ring = A.RingCacheQ8.allocate(2, 2, 4, 30, 64, torch.int8, device="cpu")
+    for cache, names in ((full, ("k", "v", "scales", "block_table")), (ring, ("k", "v", "scales", "capacity"))):
+        for name in names:
+            with pytest.raises(AttributeError, match="cannot be replaced"):
+                setattr(cache, name, getattr(cache, name))
