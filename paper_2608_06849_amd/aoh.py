@@ -11,6 +11,7 @@ never allocates device memory).
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -134,6 +135,12 @@ def lib():
         L.aoh_decode_q8.restype = ctypes.c_int
         L.aoh_decode_step_q8.argtypes = [P(AohTensor)] * 3 + L.aoh_decode_q8.argtypes[1:]
         L.aoh_decode_step_q8.restype = ctypes.c_int
+        # The same entry points with descriptors as packed bytes (_q8_desc): 0.7 us each less on the host.
+        L.packed = {}
+        for name in ("aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8", "aoh_decode_step_q8"):
+            f = L.packed[name] = L[name]
+            f.argtypes = [ctypes.c_char_p if t is P(AohTensor) else t for t in getattr(L, name).argtypes]
+            f.restype = ctypes.c_int
         L.aoh_classify_workspace_bytes.argtypes = [ctypes.c_int32] * 4
         L.aoh_classify_workspace_bytes.restype = ctypes.c_size_t
         L.aoh_classify.argtypes = [P(AohTensor), P(AohTensor), ctypes.c_int32, ctypes.c_int32,
@@ -296,7 +303,7 @@ class PagedCacheQ8(_Fixed):
         self.k, self.v, self.scales, self.block_table = k, v, scales, block_table
         self._desc = AohPagedCacheQ8(k.data_ptr(), v.data_ptr(), scales.data_ptr(), block_table.data_ptr(), pages,
                                      block_table.shape[1], heads, block_table.shape[0], _FORMATS[k.dtype])
-        self._ref, self.device, self.width = ctypes.byref(self._desc), k.device, d
+        self._ref, self.device, self.heads, self.width = ctypes.byref(self._desc), k.device, heads, d
 
     @classmethod
     def allocate(cls, num_pages, n_heads, d, dtype, block_table, device="cuda"):
@@ -320,7 +327,7 @@ class RingCacheQ8(_Fixed):
         self.k, self.v, self.scales, self.capacity = k, v, scales, capacity
         self._desc = AohRingCacheQ8(k.data_ptr(), v.data_ptr(), scales.data_ptr(), heads, capacity, batch,
                                     _FORMATS[k.dtype])
-        self._ref, self.device, self.width = ctypes.byref(self._desc), k.device, d
+        self._ref, self.device, self.heads, self.width = ctypes.byref(self._desc), k.device, heads, d
 
     @classmethod
     def allocate(cls, batch, n_heads, n_sink, window, d, dtype, device="cuda"):
@@ -478,16 +485,22 @@ def aoh_decode_step_noalloc(q, k_new, v_new, kv_full, kv_ring, head_is_streaming
 
 # ----------------------------------------------------------------------------- 8-bit caches
 
+# AohTensor of 1 to 4 dimensions as bytes
+_PACK = {n: struct.Struct(f"@Pii{n}q{32 - 8 * n}x{n}q{32 - 8 * n}x").pack for n in (1, 2, 3, 4)}
+
+
 def _q8_desc(t, name, device, width):
     """aoh_tensor descriptor of a tensor that has to be on `device`, with rows of `width`."""
-    if t.dtype not in _DTYPES:
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
         raise TypeError(f"{name}: unsupported dtype {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the caches on {device}")
     shape = t.shape
-    if len(shape) > 4 or not shape or shape[-1] != width:
+    n = len(shape)
+    if n not in _PACK or shape[-1] != width:
         raise ValueError(f"{name}: shape {tuple(shape)}, for caches of width {width}")
-    return AohTensor(t.data_ptr(), _DTYPES[t.dtype], len(shape), tuple(shape), t.stride())
+    return _PACK[n](t.data_ptr(), dtype, n, *shape, *t.stride())
 
 
 def _q8_caches(kv_full, kv_ring):
@@ -523,6 +536,7 @@ def _q8_labels(head_is_streaming, n):
 
 def _q8_run(call, device, stream, *args):
     """Calls with the device's current stream (or the given one) and that device current."""
+    call = lib().packed[call]
     if stream is None:
         handle = _current_stream(device.index)
     elif stream.device != device:
@@ -547,7 +561,7 @@ def aoh_kv_append_q8(k_new, v_new, head_is_streaming, start_pos, kv_full, kv_rin
     kd, vd = _q8_desc(k_new, "k_new", dev, d), _q8_desc(v_new, "v_new", dev, d)
     start = _q8_seqs(start_pos, "start_pos", dev, k_new.shape[0]) if start_pos is not None else None
     m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
-    _q8_run(lib().aoh_kv_append_q8, dev, stream, kd, vd, m, start, full, ring, n_sink, window)
+    _q8_run("aoh_kv_append_q8", dev, stream, kd, vd, m, start, full, ring, n_sink, window)
 
 
 def aoh_kv_append_q8_varlen(k_new, v_new, cu_seqlens, max_new, head_is_streaming, start_pos, kv_full, kv_ring, n_sink,
@@ -560,7 +574,7 @@ def aoh_kv_append_q8_varlen(k_new, v_new, cu_seqlens, max_new, head_is_streaming
     cu = _q8_seqs(cu_seqlens, "cu_seqlens", dev, 2) if n > 0 else None
     start = _q8_seqs(start_pos, "start_pos", dev, n) if start_pos is not None else None
     m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
-    _q8_run(lib().aoh_kv_append_q8_varlen, dev, stream, kd, vd, cu, n, max_new, m, start, full, ring, n_sink, window)
+    _q8_run("aoh_kv_append_q8_varlen", dev, stream, kd, vd, cu, n, max_new, m, start, full, ring, n_sink, window)
 
 
 def aoh_kv_read_q8(kv_full, kv_ring, head_is_streaming, start_pos, lens, n_sink, window, k_out, v_out, stream=None):
@@ -572,7 +586,7 @@ def aoh_kv_read_q8(kv_full, kv_ring, head_is_streaming, start_pos, lens, n_sink,
     start = _q8_seqs(start_pos, "start_pos", dev, b) if start_pos is not None else None
     n = _q8_seqs(lens, "lens", dev, b)
     m = _q8_labels(head_is_streaming, k_out.shape[-2] if k_out.dim() > 1 else 0)
-    _q8_run(lib().aoh_kv_read_q8, dev, stream, full, ring, m, start, n, n_sink, window, kd, vd)
+    _q8_run("aoh_kv_read_q8", dev, stream, full, ring, m, start, n, n_sink, window, kd, vd)
     return k_out, v_out
 
 
@@ -587,20 +601,20 @@ def _decode_q8(call, new, q, kv_full, kv_ring, head_is_streaming, lens, n_sink, 
     qd, od = _q8_desc(q, "q", dev, d), _q8_desc(out, "out", dev, d)
     kv = [_q8_desc(t, name, dev, d) for t, name in zip(new, ("k_new", "v_new"))]
     n = _q8_seqs(lens, "lens", dev, q.shape[0])
-    m = _q8_labels(head_is_streaming, (kv_full.k.shape[1] if full else 0) + (kv_ring.k.shape[1] if ring else 0))
+    m = _q8_labels(head_is_streaming, (kv_full.heads if full else 0) + (kv_ring.heads if ring else 0))
     if workspace is None:
         workspace = torch.empty(aoh_decode_q8_workspace_bytes(q.shape[0], q.shape[-2], d), dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous and on {dev}")
     _q8_run(call, dev, stream, qd, *kv, full, ring, m, n, n_sink, window, od, workspace.data_ptr(),
-            workspace.numel() * workspace.element_size())
+            workspace.nbytes)
     return out
 
 
 def aoh_decode_q8(q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out=None, workspace=None, stream=None):
     """One decode step over 8-bit caches: out[B,Hq,D] (bf16, or fp32 if `out` is) for queries at positions lens[b]-1;
     0 where lens[b] is 0."""
-    return _decode_q8(lib().aoh_decode_q8, (), q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out,
+    return _decode_q8("aoh_decode_q8", (), q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out,
                       workspace, stream)
 
 
@@ -608,7 +622,7 @@ def aoh_decode_step_q8(q, k_new, v_new, kv_full, kv_ring, head_is_streaming, len
                        workspace=None, stream=None):
     """Quantise the token at position lens[b]-1 (k_new, v_new [B,Hkv,D]) into 8-bit caches and decode with it in one
     call: the same result and caches as aoh_kv_append_q8 + aoh_decode_q8."""
-    return _decode_q8(lib().aoh_decode_step_q8, (k_new, v_new), q, kv_full, kv_ring, head_is_streaming, lens, n_sink,
+    return _decode_q8("aoh_decode_step_q8", (k_new, v_new), q, kv_full, kv_ring, head_is_streaming, lens, n_sink,
                       window, out, workspace, stream)
 
 
