@@ -86,7 +86,7 @@ struct Q8Body {
   static constexpr bool kScores = false;
   static constexpr int kWaves = WAVES;
   static constexpr int kPerSimd = PER_SIMD;
-  // 300 sequences of up to 900 tokens: 64 us (68 with 4, 66 with 12); 96 of 200-8000: 100 (102, 101).
+  // 300 sequences of up to 900 tokens: 56 us (63 with 4, 57 with 12); 96 of 200-8000: 100 (102, 101).
   static constexpr int kItemCost = 8;
   static constexpr int kBlocks = BLOCKS;
   static __device__ __forceinline__ int dim(int t, int G) { return 64 * (t >> 2) + 16 * G + 4 * (t & 3); }
@@ -343,7 +343,7 @@ namespace {
 // 64, work-space pass: two of six waves with chunks of 4 KB (16 x 131072 tokens, 4 of
 // 8 heads streaming, e4m3: 202 us; 220 with four waves and 8 KB, 218 with eight and
 // 4 KB, 236 with four and 4 KB).  The pass for many items keeps four waves, since
-// more of them cut the items further (300 sequences of up to 900 tokens: 70 us, 104
+// more of them cut the items further (300 sequences of up to 900 tokens: 57 us, 87
 // with six waves).
 template <int D, bool I8, bool WHOLE>
 void launch_body(const DecodeArgs& a, hipStream_t s) {

@@ -130,6 +130,16 @@ def test_batches_of_both_split_passes(batch, labels, hq, fmt):
     run.check(run.decode(), what="bf16 out")
 
 
+@pytest.mark.parametrize("batch,full", [(200, [70, 71, 127, 193, 199]), (129, [128]), (128, [0]), (300, []), (1024, [63, 64, 1023])])
+def test_batches_with_long_empty_stretches(batch, full):
+    lens = [0] * batch
+    for i in full:
+        lens[i] = 5 + 37 * (i % 7)
+    run = Run(4, [0, 1], 64, 4, 60, lens, q8.I8, 7, tail=1)
+    run.check(run.decode(torch.float32))
+    step_and_two_calls(run, BF)
+
+
 def test_more_sequences_than_a_launch_takes():
     r = np.random.default_rng(5)
     run = Run(2, [0, 1], 64, 4, 28, r.integers(0, 40, 2100).tolist(), q8.I8, 6, tail=1)
