@@ -413,15 +413,16 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
   constexpr int kWaves = Body::kWaves;
   constexpr int kItemCost = Body::kItemCost;
   constexpr int kPieces = 2 * kWaves;
-  constexpr int kPer = (kDimBlocks + kWaves - 1) / kWaves;  // dimension blocks of a wave in the join
   __shared__ f32x4 s_acc[kPieces][kDimBlocks][kWave];
   __shared__ float s_m[kPieces][16], s_l[kPieces][16];
   __shared__ int s_g[kPieces];  // a place of the piece's segment; -1: no piece
+  __shared__ i32x4 s_starts;
   __shared__ ManyTables<kWaves> tb;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & (kWave - 1);
   const int col = lane & 15, G = lane >> 4;
   if (threadIdx.x < kPieces) s_g[threadIdx.x] = -1;
+  if (threadIdx.x == 0) s_starts = i32x4{0, 0, 0, 0};
   const ManyPlan p = many_plan<kWaves, kItemCost>(a, tb);
   const int w = blockIdx.x;
 
@@ -433,9 +434,6 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
     g0 = min(p.g_young + (w - p.n_old) * p.r_young, p.total);
     g1 = w < p.n_old + p.n_young ? min(g0 + p.r_young, p.total) : g0;
   }
-  // the item shared with later workgroups that starts here: number of
-  // workgroups (0: none), sequence, first query head, whether a ring
-  i32x4 starts = {0, 0, 0, 0};
   const int share = ((g1 - g0 + kWaves - 1) / kWaves + 1) & ~1;  // whole 32-token chunks
   const int e1 = min(g1, g0 + share * (wave + 1));
   for (int g = min(g1, g0 + share * wave); g < e1;) {
@@ -479,46 +477,46 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
   }
   __syncthreads();
 
-  // The pieces, item by item.  Each wave combines a share of the dimension
-  // blocks.  All statistics are read at once and the loops over the pieces are
-  // unrolled (as loops with LDS reads in them they took 1.5 us more).
+  // The pieces of an item are joined by the wave that has the first of them: one item
+  // a wave, two where the workgroup's range starts inside one (300 sequences of
+  // 100-1000 tokens, width 64: 41.5 us a step, 43.9 with the waves sharing the
+  // dimensions of one item after the other).  All statistics are read at once and the
+  // loops over the pieces are unrolled (as loops with LDS reads in them they took 1.5 us more).
+  const int g_l = s_g[lane & (kPieces - 1)];
   int g_q[kPieces];
   float m_q[kPieces], l_q[kPieces];
-  {
-    const int g_l = s_g[lane & (kPieces - 1)];
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-      g_q[q] = __builtin_amdgcn_readlane(g_l, q);
-      m_q[q] = s_m[q][col];
-      l_q[q] = s_l[q][col];
-    }
+  for (int q = 0; q < kPieces; ++q) {
+    g_q[q] = __builtin_amdgcn_readlane(g_l, q);
+    m_q[q] = s_m[q][col];
+    l_q[q] = s_l[q][col];
   }
-  for (int from = 0;;) {
-    int at = INT32_MAX;
-#pragma unroll
-    for (int q = kPieces - 1; q >= 0; --q)
-      if (g_q[q] >= from) at = g_q[q];
-    if (at == INT32_MAX) break;
+  for (int mine = 2 * wave; mine < 2 * wave + 2; ++mine) {
+    const int at = __builtin_amdgcn_readlane(g_l, mine);
+    if (at < 0) continue;
     const ManyItem it = many_item<kWaves, kItemCost>(a, at, p, tb);
     const int end = it.off + it.len + kItemCost;
-    from = end;
+    bool first_here = true;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q)
+    for (int q = 0; q < kPieces; ++q) {
+      if (g_q[q] >= it.off && g_q[q] < at) first_here = false;
       if (g_q[q] >= at && g_q[q] < end) M = fmaxf(M, m_q[q]);
-    f32x4 o[kPer];
+    }
+    if (!first_here) continue;
+    f32x4 o[kDimBlocks];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int nb = 0; nb < kDimBlocks; ++nb) o[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
       if (!(g_q[q] >= at && g_q[q] < end)) continue;  // uniform
       const float wt = m_q[q] == -INFINITY ? 0.f : fast_exp2(m_q[q] - M);
       L += wt * l_q[q];
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        const f32x4 y = s_acc[q][min(wave * kPer + k, kDimBlocks - 1)][lane];
+      for (int nb = 0; nb < kDimBlocks; ++nb) {
+        const f32x4 y = s_acc[q][nb][lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[k][i] += wt * y[i];
+        for (int i = 0; i < 4; ++i) o[nb][i] += wt * y[i];
       }
     }
     const int first = many_wg_of(it.off + kItemCost, p);
@@ -528,18 +526,17 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
       const int64_t row = (int64_t)many_slot(first, w - first) * a.gs + col;
       const float inv = 1.f / L;
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        if (kPer * kWaves > kDimBlocks && wave * kPer + k >= kDimBlocks) break;
-        const int d = Body::dim(wave * kPer + k, G);
+      for (int nb = 0; nb < kDimBlocks; ++nb) {
+        const int d = Body::dim(nb, G);
         if (ns > 1) {
-          *reinterpret_cast<f32x4*>(a.part_acc + row * D + d) = o[k];
+          *reinterpret_cast<f32x4*>(a.part_acc + row * D + d) = o[nb];
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[k][i] *= inv;
-          store_out4(a, it.b, hq0 + col, d, o[k]);
+          for (int i = 0; i < 4; ++i) o[nb][i] *= inv;
+          store_out4(a, it.b, hq0 + col, d, o[nb]);
         }
       }
-      if (wave == 0 && G == 0) {
+      if (G == 0) {
         if (ns > 1) {
           a.part_ml[row * 2 + 0] = M;
           a.part_ml[row * 2 + 1] = L;
@@ -548,9 +545,12 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_m
         }
       }
     }
-    if (w == first && ns > 1) starts = i32x4{ns, it.b, hq0, it.ring};
+    // the item shared with later workgroups that starts here: number of
+    // workgroups (0: none), sequence, first query head, whether a ring
+    if (w == first && ns > 1 && lane == 0) s_starts = i32x4{ns, it.b, hq0, it.ring};
   }
-  if (threadIdx.x == 0) *reinterpret_cast<i32x4*>(a.ws_items + 4 * w) = starts;
+  __syncthreads();
+  if (threadIdx.x == 0) *reinterpret_cast<i32x4*>(a.ws_items + 4 * w) = s_starts;
 
   // Rows without a key.
   for (int b = w; b < a.B; b += gridDim.x) {
