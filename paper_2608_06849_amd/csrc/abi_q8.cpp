@@ -95,19 +95,19 @@ size_t decode_need(int64_t batch, int64_t hq, int64_t d) {
 
 // Whether a step is split by the pass for many items (decode_split.h), which
 // starts later (its tables) but holds whole items, so it saves partials at every
-// item.  us a step, many / work-space pass, half of the heads streaming, window 512.
-// Width 128, 128 items: of four heads 27 / 30 (300-6000 tokens), 63 / 66
-// (2000-30000), of one 26 / 25, 62 / 63, of seven 28 / 34; 64 items of four 22 / 20.
-// Width 64, 128 items of four 20 / 20, 41 / 39, of one 20 / 18, 40 / 37; 256 of four
-// 26 / 30, 63 / 66, of one 26 / 26, 62 / 62, 512 of one 38 / 44.
+// item.  us a step, work-space pass / many, half of the heads streaming, window 512.
+// Width 128, 64 items of four heads 20.1 / 22.9 (300-6000 tokens), 39.9 / 43.2
+// (2000-30000), 128 items 29.8 / 26.8, 66.0 / 63.6, of one head 25.5 / 25.5, 62.3 / 62.6,
+// of seven 34.4 / 27.8, 72.3 / 65.0.  Width 64, 64 items of four 14.6 / 18.0,
+// 24.6 / 28.6, 128 of four 19.8 / 18.4, 39.2 / 39.2, of one 18.1 / 17.9, 38.2 / 38.4, of seven
+// 22.2 / 19.6, 42.5 / 40.3.
 // In caches of 32 blocks and fewer no item is in many workgroups, which the pass for
-// many items would merge one after the other (200-500 tokens): width 128, 32 items of
-// seven heads 12.5 / 13.5, of four 12.0 / 12.1, 64 of one 12.7 / 12.5; width 64, 128
-// of four 11.9 / 13.2, 64 of four 11.6 / 10.6, 128 of one 11.8 / 11.3.
-bool takes_many(int64_t B, int64_t Hkv, int gs, int D, int64_t blocks) {
+// many items would merge one after the other (200-400 tokens, window 256): width 128, 32
+// items of four 12.1 / 11.5, of one 11.7 / 11.2, of seven 13.5 / 12.2; width 64, 32 of four
+// 10.1 / 10.4, 64 of four 10.6 / 10.6, of one 10.2 / 10.4, of seven 12.0 / 10.9.
+bool takes_many(int64_t B, int64_t Hkv, int D, int64_t blocks) {
   if (B > kWsMaxBatch) return true;
-  int64_t many = D == 128 ? 128 : 256;
-  if (blocks <= 32 && gs >= 4) many = D == 128 ? 32 : 128;
+  const int64_t many = blocks > 32 ? 128 : D == 128 ? 32 : 64;
   return B * Hkv >= many;
 }
 
@@ -196,7 +196,7 @@ aoh_status decode_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
     }
     a.ws_cu = cu;
     int64_t rows = (2 * cu + nb * Hkv) * gs;
-    if (takes_many(nb, Hkv, gs, (int)D, blocks)) {
+    if (takes_many(nb, Hkv, (int)D, blocks)) {
       a.many_wgs = 2 * cu;
       rows = (int64_t)4 * cu * gs;
     }
