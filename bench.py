@@ -127,8 +127,8 @@ TRAFFIC = {
     "write_factor": 1048576.0 / 1048576.0,  # WRITE_SIZE of a 1 GiB copy / 1 GiB
     "prefill_mixed": {"fetch_kib": 465775.0, "write_kib": 263396.3,
                       "sources": PREFILL_SOURCES, "source_hash": "f5ebfbb1542746d2"},
-    "decode_ws": {"fetch_kib": 1081204.8, "write_kib": 1169.8,
-                  "sources": DECODE_SOURCES, "source_hash": "78d1ea59a23b0c0b"},
+    "decode_ws": {"fetch_kib": 1082956.1, "write_kib": 1169.8,
+                  "sources": DECODE_SOURCES, "source_hash": "f7e8359f719e01bf"},
 }
 
 

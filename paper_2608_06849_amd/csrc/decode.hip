@@ -459,6 +459,7 @@ struct Bf16Body {
   static constexpr int kWaves = kSplitWaves;
   static constexpr int kPerSimd = 2;
   static constexpr int kItemCost = 4;
+  static constexpr int kWsItemCost = 0;  // another one would move the ranges, and with them roundings
   static __device__ __forceinline__ void run(const DecodeArgs& a, bool ring, int b, int kvl, int len, int blk0,
                                              int blk_lim, f32x4 (&acc)[D / 16], float& m, float& l, void* lds) {
     if (ring) decode_split_body<D, true, false, MODE == 3>(a, a.ring, b, kvl, len, blk0, blk_lim, acc, m, l);

@@ -7,6 +7,8 @@
 //   kD, kScores                      width; whether scores are kept (anchor layer)
 //   kWaves, kPerSimd                 waves of a workgroup, and of a SIMD
 //   kItemCost                        what starting a segment costs a wave, in blocks
+//                                    (decode_many_kernel)
+//   kWsItemCost                      what it costs a workgroup (decode_ws_kernel)
 //   run(a, ring, b, kvl, len, blk0, blk_lim, acc, m, l, lds)
 //     blocks [blk0, blk_lim) of the ring or paged cache row of (sequence b, KV head
 //     kvl): the unnormalised sums acc (0 before), the maximum m in log2 units and
@@ -98,7 +100,9 @@ __device__ __forceinline__ void merge_waves_store(const DecodeArgs& a, f32x4 (&a
 // Work space: the valid 16-token blocks of every item (cache type, sequence,
 // KV head) laid end to end, paged items first, each type in (sequence, KV
 // head) order, so one plan covers any mix of lengths and of the two cache
-// types.  Each workgroup takes one contiguous range of it and each of its
+// types.  Every item is preceded by kWsItemCost places without a block, so that
+// ranges of short items, which a workgroup takes one after the other, hold few of
+// them.  Each workgroup takes one contiguous range of it and each of its
 // waves a consecutive share of every item segment in that range; the waves'
 // states are merged in LDS and the workgroup writes one partial per segment.
 // The launch has two workgroups per CU: the first n_cu are placed one per CU,
@@ -124,17 +128,18 @@ __device__ __forceinline__ int ws_n_wg(int total, int n_cu, int max_wg) {
 }
 
 struct WsPlan {
-  int nb_tot, nbr_tot;  // paged / ring blocks summed over the sequences
-  int total;            // blocks of all items
+  int nb_tot, nbr_tot;  // paged / ring places summed over the sequences
+  int total;            // places of all items
   int n_old, n_young;   // workgroups of the first and second round
-  int r_old, r_young;   // blocks per range of each round
-  int g_young;          // first block of the second round's ranges
+  int r_old, r_young;   // places per range of each round
+  int g_young;          // first place of the second round's ranges
 };
 
 // The plan from the sequence lengths.  Every lane of a wave calls it; lane b
-// gets sequence b's length, its valid block counts in the paged cache (nb)
-// and the ring (nbr), and their exclusive prefix sums over the sequences
+// gets sequence b's length, its places (blocks + COST, 0 without blocks) in the paged
+// cache (nb) and the ring (nbr), and their exclusive prefix sums over the sequences
 // (P, Q); lanes >= B get zeros.
+template <int COST>
 __device__ __forceinline__ WsPlan ws_plan(const int32_t* lens, int B, int max_pages, int n_ret, int ring_cap,
                                           int n_str, int n_cu, int& len, int& nb, int& nbr, int& P, int& Q) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -146,6 +151,8 @@ __device__ __forceinline__ WsPlan ws_plan(const int32_t* lens, int B, int max_pa
     const int l = max(len, 0);
     if (n_ret) nb = (min(l, max_pages * kPage) + kPage - 1) / kPage;
     if (n_str) nbr = (min(l, ring_cap) + kPage - 1) / kPage;
+    nb += nb ? COST : 0;
+    nbr += nbr ? COST : 0;
   }
   int ip = nb, iq = nbr;
 #pragma unroll
@@ -172,18 +179,19 @@ __device__ __forceinline__ WsPlan ws_plan(const int32_t* lens, int B, int max_pa
   return p;
 }
 
-// Workgroup whose range holds block g (g < total).
+// Workgroup whose range holds place g (g < total).
 __device__ __forceinline__ int ws_wg_of(int g, const WsPlan& p) {
   return g < p.g_young ? g / p.r_old : p.n_old + (g - p.g_young) / p.r_young;
 }
 
-// The item holding block g of the work space (g < total): its type, sequence,
-// KV head rank, first block in the work space, valid blocks and item index.
+// The item holding place g of the work space (g < total): its type, sequence,
+// KV head rank, first place in the work space, valid blocks and item index.
 struct WsItem {
   bool ring;
   int b, kvl, off, len, idx;
 };
 
+template <int COST>
 __device__ __forceinline__ WsItem ws_item(int g, const WsPlan& p, int B, int n_ret, int n_str, int nb, int nbr, int P,
                                           int Q) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -200,9 +208,10 @@ __device__ __forceinline__ WsItem ws_item(int g, const WsPlan& p, int B, int n_r
   }
   it.b = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
   const int first = __builtin_amdgcn_readlane(start, it.b);
-  it.len = __builtin_amdgcn_readlane(blocks, it.b);
-  it.kvl = (g - first) / it.len;
-  it.off = first + it.kvl * it.len;
+  const int places = __builtin_amdgcn_readlane(blocks, it.b);
+  it.kvl = (g - first) / places;
+  it.off = first + it.kvl * places;
+  it.len = places - COST;
   it.idx = it.ring ? B * n_ret + it.b * n_str + it.kvl : it.b * n_ret + it.kvl;
   return it;
 }
@@ -220,7 +229,8 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_w
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & (kWave - 1);
   int len_l, nb_l, nbr_l, P_l, Q_l;
-  const WsPlan p = ws_plan(a.lens, a.B, a.full.max_pages, a.full.n_kv, a.ring_cap, a.ring.n_kv, a.ws_cu, len_l, nb_l,
+  constexpr int kCost = Body::kWsItemCost;
+  const WsPlan p = ws_plan<kCost>(a.lens, a.B, a.full.max_pages, a.full.n_kv, a.ring_cap, a.ring.n_kv, a.ws_cu, len_l, nb_l,
                            nbr_l, P_l, Q_l);
   const int w = blockIdx.x;
   int g0, g1;
@@ -232,9 +242,11 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_w
     g1 = w < p.n_old + p.n_young ? min(g0 + p.r_young, p.total) : g0;
   }
   for (int g = g0; g < g1;) {  // uniform: every wave walks the same segments
-    const WsItem it = ws_item(g, p, a.B, a.full.n_kv, a.ring.n_kv, nb_l, nbr_l, P_l, Q_l);
+    const WsItem it = ws_item<kCost>(g, p, a.B, a.full.n_kv, a.ring.n_kv, nb_l, nbr_l, P_l, Q_l);
     if (it.len == 0) break;
-    const int s0 = g - it.off, s1 = min(g1 - it.off, it.len);
+    const int s0 = max(0, g - it.off - kCost), s1 = min(g1 - it.off - kCost, it.len);
+    g = it.off + kCost + s1;
+    if (s0 >= s1) break;  // only places before the item's blocks: the range ends here
     const int len = __builtin_amdgcn_readlane(len_l, it.b);
     // This wave's consecutive share of the segment's 32-token chunks.
     const int per = ((s1 - s0 + 1) / 2 + kWaves - 1) / kWaves;
@@ -250,9 +262,8 @@ __global__ __launch_bounds__(Body::kWaves * kWave, Body::kPerSimd) void decode_w
       // The workgroup holding the item's first block records where the item's
       // partials are for the merge pass: first slot and count.
       a.ws_items[2 * it.idx + 0] = w + it.idx;
-      a.ws_items[2 * it.idx + 1] = ws_wg_of(it.off + it.len - 1, p) - w + 1;
+      a.ws_items[2 * it.idx + 1] = ws_wg_of(it.off + kCost + it.len - 1, p) - w + 1;
     }
-    g = it.off + s1;
   }
 }
 

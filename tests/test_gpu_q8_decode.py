@@ -154,6 +154,14 @@ def test_one_long_sequence_is_split(d, length):
     run.check(run.decode(torch.float32))
 
 
+@pytest.mark.parametrize("lens", [[1, 3000], [2500] + [1] * 20, [0, 17, 0, 1, 1900, 16], [40] * 30])
+@pytest.mark.parametrize("hq,labels,d", [(8, [0] * 8, 64), (6, [1, 0, 1], 128), (2, [1, 1], 128)])
+def test_short_and_long_sequences_together(hq, labels, d, lens):
+    run = Run(hq, labels, d, 4, 1500, lens, q8.E4M3, 12, tail=1)
+    run.check(run.decode(torch.float32))
+    step_and_two_calls(run, BF)
+
+
 def test_lengths_beyond_the_table_are_clamped():
     run = Run(2, [0], 64, 0, 1, [64, 32], q8.I8, 10, extra_pages=0)
     full = PagedCacheQ8(run.full.k, run.full.v, run.full.scales, run.full.block_table[:, :2].contiguous())
