@@ -93,22 +93,24 @@ size_t decode_need(int64_t batch, int64_t hq, int64_t d) {
   return std::max(ws_bytes(kWsMaxWgs * gs + few * hq, 2 * few * hq, d), ws_bytes(2 * kWsMaxWgs * gs, 4 * kWsMaxWgs, d));
 }
 
-// Whether a step is split by the pass for many items (decode_split.h), which
-// starts later (its tables) but holds whole items, so it saves partials at every
-// item.  us a step, work-space pass / many, half of the heads streaming, window 512.
-// Width 128, 64 items of four heads 20.1 / 22.9 (300-6000 tokens), 39.9 / 43.2
-// (2000-30000), 128 items 29.8 / 26.8, 66.0 / 63.6, of one head 25.5 / 25.5, 62.3 / 62.6,
-// of seven 34.4 / 27.8, 72.3 / 65.0.  Width 64, 64 items of four 14.6 / 18.0,
-// 24.6 / 28.6, 128 of four 19.8 / 18.4, 39.2 / 39.2, of one 18.1 / 17.9, 38.2 / 38.4, of seven
-// 22.2 / 19.6, 42.5 / 40.3.
-// In caches of 32 blocks and fewer no item is in many workgroups, which the pass for
-// many items would merge one after the other (200-400 tokens, window 256): width 128, 32
-// items of four 12.1 / 11.5, of one 11.7 / 11.2, of seven 13.5 / 12.2; width 64, 32 of four
-// 10.1 / 10.4, 64 of four 10.6 / 10.6, of one 10.2 / 10.4, of seven 12.0 / 10.9.
-bool takes_many(int64_t B, int64_t Hkv, int D, int64_t blocks) {
+// Whether a step is split by the pass for many items (decode_split.h), which starts
+// later (its tables) and merges the workgroups of an item one after the other, but
+// holds whole items, so it saves partials (of all query heads) at every item.  us a
+// step, work-space pass / many, half of the heads streaming, window 512, 300-6000 tokens
+// a sequence, then 2000-30000.  Width 128, 64 items of four heads 18.1 / 23.0, 37.6 / 43.0,
+// 128 of four 27.9 / 26.9, 63.5 / 63.8, of seven 33.0 / 27.7, 68.4 / 65.1, 256 of one
+// 35.8 / 36.6, 104.9 / 105.8, of two 39.0 / 36.8, 108.2 / 105.2, 32 of sixteen 22.1 / 33.8,
+// 41.5 / 56.7.  Width 64, 128 of four 17.7 / 18.5, 37.6 / 38.9, 256 of one 22.6 / 23.9,
+// 60.0 / 60.4, of four 27.2 / 24.5, 64.7 / 60.3, of two 24.2 / 24.1, 61.6 / 60.0.
+// In caches of 32 blocks and fewer no item is in many workgroups (200-400 tokens,
+// window 256).  Width 128, 64 items of four heads 11.6 / 12.3, of seven 14.1 / 12.7, 60 of eight
+// 14.7 / 12.9, 32 of sixteen 14.9 / 15.1, 128 of four 17.3 / 13.2; width 64, 64 of seven
+// 10.6 / 11.0, 60 of sixteen 13.9 / 11.2, 128 of four 11.8 / 10.7.
+bool takes_many(int64_t B, int64_t Hkv, int gs, int D, int64_t blocks) {
   if (B > kWsMaxBatch) return true;
-  const int64_t many = blocks > 32 ? 128 : D == 128 ? 32 : 64;
-  return B * Hkv >= many;
+  const int64_t items = B * Hkv;
+  if (blocks <= 32) return items >= 48 && items * gs >= 448;
+  return items >= (D == 128 ? 128 : 256) && items * gs >= 512;
 }
 
 aoh_status decode_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new, bool step,
@@ -196,7 +198,7 @@ aoh_status decode_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
     }
     a.ws_cu = cu;
     int64_t rows = (2 * cu + nb * Hkv) * gs;
-    if (takes_many(nb, Hkv, (int)D, blocks)) {
+    if (takes_many(nb, Hkv, gs, (int)D, blocks)) {
       a.many_wgs = 2 * cu;
       rows = (int64_t)4 * cu * gs;
     }
