@@ -7,7 +7,8 @@ library's HIP kernels.  If libaoh.so is missing or cannot be loaded, every call
 raises: there is no fallback path.
 
 Cache helpers allocate the two cache layouts with torch (the library itself
-never allocates device memory).
+never allocates device memory); what the 8-bit caches' calls allocate for a
+given stream belongs to that stream.
 """
 import ctypes
 import os
@@ -214,6 +215,23 @@ def _stream(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _scratch(stream, make, *args, **kw):
+    """Memory for a call on `stream` (None: the current one), as `make(*args, **kw)` gives it.  It belongs to that stream,
+    so that its block goes to later work of that stream only, also when it is freed before the call's kernels have run."""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
+def _result(stream, make, *args, **kw):
+    """The same for a tensor that the caller gets: where it is freed, its block also waits for the caller's stream."""
+    t = _scratch(stream, make, *args, **kw)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
 
 
 def _ptr(t):
@@ -596,14 +614,16 @@ def aoh_decode_q8_workspace_bytes(batch, n_q_heads, d_head):
 
 def _decode_q8(call, new, q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out, workspace, stream):
     dev, d, full, ring = _q8_caches(kv_full, kv_ring)
+    qd = _q8_desc(q, "q", dev, d)
     if out is None:
-        out = torch.empty_like(q)
-    qd, od = _q8_desc(q, "q", dev, d), _q8_desc(out, "out", dev, d)
+        out = _result(stream, torch.empty_like, q)
+    od = _q8_desc(out, "out", dev, d)
     kv = [_q8_desc(t, name, dev, d) for t, name in zip(new, ("k_new", "v_new"))]
     n = _q8_seqs(lens, "lens", dev, q.shape[0])
     m = _q8_labels(head_is_streaming, (kv_full.heads if full else 0) + (kv_ring.heads if ring else 0))
     if workspace is None:
-        workspace = torch.empty(aoh_decode_q8_workspace_bytes(q.shape[0], q.shape[-2], d), dtype=torch.uint8, device=dev)
+        workspace = _scratch(stream, torch.empty, aoh_decode_q8_workspace_bytes(q.shape[0], q.shape[-2], d),
+                             dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous and on {dev}")
     _q8_run(call, dev, stream, qd, *kv, full, ring, m, n, n_sink, window, od, workspace.data_ptr(),
