@@ -7,8 +7,8 @@ library's HIP kernels.  If libaoh.so is missing or cannot be loaded, every call
 raises: there is no fallback path.
 
 Cache helpers allocate the two cache layouts with torch (the library itself
-never allocates device memory); what the 8-bit caches' calls allocate for a
-given stream belongs to that stream.
+never allocates device memory); what a call on a given stream allocates
+belongs to that stream.
 """
 import ctypes
 import os
@@ -381,7 +381,7 @@ def _check_i32(t, name, device):
 def aoh_prefill(q, k, v, head_is_streaming, n_sink, window, out=None, stream=None):
     """out[B,T,Hq,D] = head-mixed causal attention (see aoh.h)."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
     m = _Mask(head_is_streaming)
     _check(lib().aoh_prefill(ctypes.byref(qd), ctypes.byref(kd), ctypes.byref(vd), m.ptr,
@@ -392,7 +392,7 @@ def aoh_prefill(q, k, v, head_is_streaming, n_sink, window, out=None, stream=Non
 def aoh_prefill_chunked(q, k, v, head_is_streaming, n_sink, window, chunk, out=None, stream=None):
     """Prefill with chunk eviction of `chunk` tokens for streaming heads (see aoh.h)."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
     m = _Mask(head_is_streaming)
     _check(lib().aoh_prefill_chunked(ctypes.byref(qd), ctypes.byref(kd), ctypes.byref(vd), m.ptr,
@@ -404,7 +404,7 @@ def aoh_prefill_append(q, k, v, head_is_streaming, n_sink, window, kv_full, kv_r
                        stream=None):
     """Prefill of a new prompt that also writes its K/V into the caches (see aoh.h)."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None
     rd = kv_ring.desc() if kv_ring is not None else None
@@ -419,7 +419,7 @@ def aoh_prefill_varlen(q, k, v, cu_seqlens, max_seqlen, head_is_streaming, n_sin
                        kv_ring=None, out=None, stream=None):
     """Packed variable-length prefill: q [total, Hq, D], k/v [total, Hkv, D], cu_seqlens device int32 [B + 1]."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None
     rd = kv_ring.desc() if kv_ring is not None else None
@@ -452,7 +452,7 @@ def aoh_decode(q, kv_full, kv_ring, head_is_streaming, lens, n_sink, window, out
                workspace=None, stream=None):
     """One decode step: out[B,Hq,D] for queries at positions lens[b]-1."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, od = tensor_desc(q), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None
     rd = kv_ring.desc() if kv_ring is not None else None
@@ -471,7 +471,7 @@ def aoh_decode_step(q, k_new, v_new, kv_full, kv_ring, head_is_streaming, lens, 
     """Append the token at position lens[b]-1 (k_new, v_new [B,Hkv,D]) and decode
     with it in one call: the same result and caches as aoh_kv_append + aoh_decode."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, kd, vd, od = tensor_desc(q), tensor_desc(k_new), tensor_desc(v_new), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None
     rd = kv_ring.desc() if kv_ring is not None else None
@@ -490,7 +490,7 @@ def aoh_decode_step_noalloc(q, k_new, v_new, kv_full, kv_ring, head_is_streaming
     """aoh_decode_step without a workspace: the library's static scratch area
     holds the split partials (calls on one GPU must not overlap)."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     qd, kd, vd, od = tensor_desc(q), tensor_desc(k_new), tensor_desc(v_new), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None
     rd = kv_ring.desc() if kv_ring is not None else None
@@ -668,14 +668,14 @@ def aoh_classify(w_q, w_k, d_head, n_retrieval, head_rank=None, group_score=None
     L, hq, hkv = w_q.shape[0], w_q.shape[1] // d_head, w_k.shape[1] // d_head
     dev = w_q.device
     if head_rank is None:
-        head_rank = torch.empty((L, hq), dtype=torch.float64, device=dev)
+        head_rank = _result(stream, torch.empty, (L, hq), dtype=torch.float64, device=dev)
     if group_score is None:
-        group_score = torch.empty((L, hkv), dtype=torch.float64, device=dev)
+        group_score = _result(stream, torch.empty, (L, hkv), dtype=torch.float64, device=dev)
     if head_is_streaming is None:
-        head_is_streaming = torch.empty((L, hkv), dtype=torch.uint8, device=dev)
+        head_is_streaming = _result(stream, torch.empty, (L, hkv), dtype=torch.uint8, device=dev)
     if workspace is None:
         n = aoh_classify_workspace_bytes(L, hq, hkv, d_head)
-        workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+        workspace = _scratch(stream, torch.empty, max(n, 16), dtype=torch.uint8, device=dev)
     qd, kd = tensor_desc(w_q), tensor_desc(w_k)
     _check(lib().aoh_classify(ctypes.byref(qd), ctypes.byref(kd), d_head, n_retrieval, _ptr(head_rank),
                               _ptr(group_score), _ptr(head_is_streaming), _ptr(workspace),
@@ -683,9 +683,9 @@ def aoh_classify(w_q, w_k, d_head, n_retrieval, head_rank=None, group_score=None
     return head_rank, group_score, head_is_streaming
 
 
-def _ws(workspace, n_bytes, device):
+def _ws(workspace, n_bytes, device, stream):
     if workspace is None:
-        workspace = torch.empty(max(n_bytes, 16), dtype=torch.uint8, device=device)
+        workspace = _scratch(stream, torch.empty, max(n_bytes, 16), dtype=torch.uint8, device=device)
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -699,10 +699,10 @@ def aoh_head_mapping(w_q_anchor, w_k_anchor, w_q_reuse, w_k_reuse, d_head, ancho
     Returns device tensors (head_sim [Hq, Hq] f64, group_sim [Hkv, Hkv] f64, mapping [Hkv] i32)."""
     hq, hkv = w_q_anchor.shape[0] // d_head, w_k_anchor.shape[0] // d_head
     dev = w_q_anchor.device
-    head_sim = torch.empty((hq, hq), dtype=torch.float64, device=dev)
-    group_sim = torch.empty((hkv, hkv), dtype=torch.float64, device=dev)
-    mapping = torch.empty(hkv, dtype=torch.int32, device=dev)
-    workspace, wsb = _ws(workspace, aoh_head_mapping_workspace_bytes(hq, hkv, d_head), dev)
+    head_sim = _result(stream, torch.empty, (hq, hq), dtype=torch.float64, device=dev)
+    group_sim = _result(stream, torch.empty, (hkv, hkv), dtype=torch.float64, device=dev)
+    mapping = _result(stream, torch.empty, hkv, dtype=torch.int32, device=dev)
+    workspace, wsb = _ws(workspace, aoh_head_mapping_workspace_bytes(hq, hkv, d_head), dev, stream)
     ds = [tensor_desc(t) for t in (w_q_anchor, w_k_anchor, w_q_reuse, w_k_reuse)]
     ma, mr = _Mask(anchor_is_streaming), _Mask(reuse_is_streaming)
     _check(lib().aoh_head_mapping(*[ctypes.byref(d) for d in ds], d_head, ma.ptr, mr.ptr, _ptr(head_sim),
@@ -718,14 +718,14 @@ def aoh_decode_anchor(q, kv_full, kv_ring, head_is_streaming, lens, n_sink, wind
                       workspace=None, stream=None):
     """Anchor-layer decode step; returns (out, indices [B, n_retrieval_groups, top_k] int32)."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     n_ret = sum(1 for x in head_is_streaming if not x)
     if indices is None:
-        indices = torch.empty((q.shape[0], max(n_ret, 1), top_k), dtype=torch.int32, device=q.device)
+        indices = _result(stream, torch.empty, (q.shape[0], max(n_ret, 1), top_k), dtype=torch.int32, device=q.device)
     max_pages = kv_full.block_table.shape[1] if kv_full is not None else 1
     cap = kv_ring.capacity if kv_ring is not None else n_sink + window
     workspace, wsb = _ws(workspace, aoh_decode_anchor_workspace_bytes(q.shape[0], q.shape[1], q.shape[2], max_pages,
-                                                                      cap), q.device)
+                                                                      cap), q.device, stream)
     qd, od = tensor_desc(q), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None
     rd = kv_ring.desc() if kv_ring is not None else None
@@ -745,11 +745,11 @@ def aoh_decode_reuse(q, kv_full, kv_ring, head_is_streaming, lens, n_sink, windo
     """Reuse-layer decode step with borrowed positions indices [B, n_lists, top_k] (device int32) and
     mapping (host sequence of Hkv list rows)."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _result(stream, torch.empty_like, q)
     n_lists, top_k = indices.shape[1], indices.shape[2]
     cap = kv_ring.capacity if kv_ring is not None else n_sink + window
     workspace, wsb = _ws(workspace, aoh_decode_reuse_workspace_bytes(q.shape[0], q.shape[1], q.shape[2], top_k, cap),
-                         q.device)
+                         q.device, stream)
     mp = (ctypes.c_int32 * len(mapping))(*[int(x) for x in mapping])
     qd, od = tensor_desc(q), tensor_desc(out)
     fd = kv_full.desc() if kv_full is not None else None

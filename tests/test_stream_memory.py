@@ -64,11 +64,26 @@ def rows(*shape, dtype=BF):
     return torch.zeros(shape, dtype=dtype)
 
 
+WQ, WK = rows(HQ * D, 128), rows(HKV * D, 128)
+PROMPT, KV = rows(1, 5, HQ, D), rows(1, 5, HKV, D)
+CU = torch.tensor([0, 5], dtype=torch.int32)
 LENS = torch.ones(B, dtype=torch.int32)
 Q, NEW = rows(B, HQ, D), rows(B, HKV, D)
 CALLS = {
     "aoh_decode_q8": lambda **kw: A.aoh_decode_q8(Q, None, None, [0, 1], LENS, 4, 28, **kw),
     "aoh_decode_step_q8": lambda **kw: A.aoh_decode_step_q8(Q, NEW, NEW, None, None, [0, 1], LENS, 4, 28, **kw),
+    "aoh_prefill": lambda **kw: A.aoh_prefill(PROMPT, KV, KV, [0, 1], 4, 28, **kw),
+    "aoh_prefill_chunked": lambda **kw: A.aoh_prefill_chunked(PROMPT, KV, KV, [0, 1], 4, 28, 32, **kw),
+    "aoh_prefill_append": lambda **kw: A.aoh_prefill_append(PROMPT, KV, KV, [0, 1], 4, 28, None, None, **kw),
+    "aoh_prefill_varlen": lambda **kw: A.aoh_prefill_varlen(PROMPT[0], KV[0], KV[0], CU, 5, [0, 1], 4, 28, **kw),
+    "aoh_decode": lambda **kw: A.aoh_decode(Q, None, None, [0, 1], LENS, 4, 28, **kw),
+    "aoh_decode_step": lambda **kw: A.aoh_decode_step(Q, NEW, NEW, None, None, [0, 1], LENS, 4, 28, **kw),
+    "aoh_decode_step_noalloc": lambda **kw: A.aoh_decode_step_noalloc(Q, NEW, NEW, None, None, [0, 1], LENS, 4, 28, **kw),
+    "aoh_classify": lambda **kw: A.aoh_classify(WQ[None], WK[None], D, 1, **kw),
+    "aoh_head_mapping": lambda **kw: A.aoh_head_mapping(WQ, WK, WQ, WK, D, [0, 1], [0, 1], **kw),
+    "aoh_decode_anchor": lambda **kw: A.aoh_decode_anchor(Q, None, None, [0, 1], LENS, 4, 28, 8, **kw),
+    "aoh_decode_reuse": lambda **kw: A.aoh_decode_reuse(Q, None, None, [0, 1], LENS, 4, 28, rows(B, 1, 8, dtype=torch.int32),
+                                                        [0, 0], **kw),
 }
 
 
