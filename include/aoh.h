@@ -404,11 +404,11 @@ size_t aoh_decode_q8_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t d
 
 /*
  * aoh_decode over 8-bit caches: softmax(q . K / sqrt(D)) V over the values that
- * the codes stand for, with q bf16 and sums in fp32.  Scales and codes enter
- * exactly; each weight is rounded to bf16 before the product with V for a bf16
- * out, and not rounded for an fp32 out.  A sequence with lens[b] <= 0
- * (an empty place of a padded batch) gets 0.  Lengths are clamped to the block
- * table's capacity.  AOH_ERR_UNSUPPORTED for fp32 q, for Hq / Hkv > 16 and for
+ * the codes stand for, with q bf16 and weights and sums in fp32.  Scales and
+ * codes enter exactly, and no weight is rounded to fewer bits before the product
+ * with V.  A sequence with lens[b] <= 0 (an empty place of a padded batch) gets
+ * 0.  Lengths are clamped to the block table's capacity.  AOH_ERR_UNSUPPORTED for
+ * fp32 q, for Hq / Hkv > 16 and for
  * Hkv * (capacity of a sequence in 16-token blocks + 16) >= 2^29.
  * Graph capture and workspace as for aoh_decode.
  */

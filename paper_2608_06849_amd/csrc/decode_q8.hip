@@ -6,11 +6,14 @@
 //   S^T[16 tokens x 16 heads] = K[16 x 32 dims] . Q^T       (D/32 steps a block)
 //   O^T[16 dims x 16 heads]  += V^T[16 dims x 32 tokens] . P^T   (D/16 a block pair)
 // with v_mfma_f32_16x16x32_bf16 on codes converted to bf16, exactly.  K's row
-// scale multiplies the scores and V's the probabilities, exactly too: only the
-// weight, probability times V's scale, is rounded to bf16, as in the bf16 caches'
-// pass, or for fp32 outputs kept whole as the sum of three bf16 numbers, which costs
-// two more products (16 sequences of 2000-32000 tokens, width 64: 41.3 us a step,
-// 39.6 with two numbers and 2^-18 of each weight lost; width 128: 0-1.5%).
+// scale multiplies the scores and V's the probabilities, exactly too.  A weight,
+// probability times V's scale, is kept whole, as the sum of three bf16 numbers, which
+// costs two more products.  us a step with weights rounded to bf16 / with two numbers
+// (2^-16 of a weight lost) / whole: 8 sequences of 131072 tokens 187.1 / 187.5 / 188.1,
+// 96 of 200-8000 91.4 / 91.9 / 92.3, one of 4093 10.1 / 10.4 / 10.5, 300 of up to 900
+// (width 64, int8) 51.7 / 53.1 / 56.0; the error of a bf16 output against float64,
+// relative to its norm, 1.68e-3 / 1.66e-3 / 1.66e-3 for the first of these, 1.89e-3 /
+// 1.62e-3 / 1.62e-3 for the last, and up to a quarter less in steps of few tokens.
 //   Bound: HBM.  8 sequences of 131072 tokens, 4 of 8 heads streaming, e4m3: 175 us
 // in the pass (1.09 GB of codes and scales, 1.03 times that fetched), 6.2 TB/s;
 // with an exponential only for every fourth score, or without converting codes, not
@@ -79,8 +82,7 @@ __device__ __forceinline__ void store_token(const DecodeArgs& a, uint8_t* uk, ui
 
 }  // namespace
 
-// WHOLE: weights unrounded, as the sums of three bf16 numbers.
-template <int D, bool I8, bool WHOLE, int WAVES, int BLOCKS, int PER_SIMD>
+template <int D, bool I8, int WAVES, int BLOCKS, int PER_SIMD>
 struct Q8Body {
   static constexpr int kD = D;
   static constexpr bool kScores = false;
@@ -159,7 +161,7 @@ struct Q8Body {
         for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
     }
     float psum = 0.f;
-    constexpr int kParts = WHOLE ? 3 : 1;
+    constexpr int kParts = 3;  // bf16 numbers of a weight
     u32x4 part[kBlocks / 2][kParts];
 #pragma unroll
     for (int X = 0; X < kBlocks; ++X)
@@ -170,18 +172,14 @@ struct Q8Body {
         w[X][i] *= p;
         if (!(i & 1)) continue;
         const int word = 2 * (X & 1) + i / 2;
-        if constexpr (WHOLE) {
-          // the upper eight bits, the next eight of what is left, the last eight
-          float w0 = w[X][i - 1], w1 = w[X][i];
+        // the upper eight bits, the next eight of what is left, the last eight
+        float w0 = w[X][i - 1], w1 = w[X][i];
 #pragma unroll
-          for (int n = 0; n < kParts; ++n) {
-            const uint32_t b0 = __builtin_bit_cast(uint32_t, w0), b1 = __builtin_bit_cast(uint32_t, w1);
-            part[X / 2][n][word] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-            w0 -= __builtin_bit_cast(float, b0 & 0xffff0000u);
-            w1 -= __builtin_bit_cast(float, b1 & 0xffff0000u);
-          }
-        } else {
-          part[X / 2][0][word] = pack_bf16(w[X][i - 1], w[X][i]);
+        for (int n = 0; n < kParts; ++n) {
+          const uint32_t b0 = __builtin_bit_cast(uint32_t, w0), b1 = __builtin_bit_cast(uint32_t, w1);
+          part[X / 2][n][word] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+          w0 -= __builtin_bit_cast(float, b0 & 0xffff0000u);
+          w1 -= __builtin_bit_cast(float, b1 & 0xffff0000u);
         }
       }
     l_run += psum;
@@ -348,21 +346,15 @@ namespace {
 // 4 KB, 236 with four and 4 KB).  The pass for many items keeps four waves, since
 // more of them cut the items further (300 sequences of up to 900 tokens: 57 us, 87
 // with six waves).
-template <int D, bool I8, bool WHOLE>
-void launch_body(const DecodeArgs& a, hipStream_t s) {
-  if (a.many_wgs) {
-    using Body = Q8Body<D, I8, WHOLE, 4, 4, 2>;
-    hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), dim3(Body::kWaves * kWave), 0, s, a);
-  } else {
-    using Body = std::conditional_t<D == 64, Q8Body<D, I8, WHOLE, 6, 2, 4>, Q8Body<D, I8, WHOLE, 4, 4, 2>>;
-    hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), dim3(Body::kWaves * kWave), 0, s, a);
-  }
-}
-
 template <int D, bool I8>
 void launch_format(const DecodeArgs& a, hipStream_t s) {
-  if (a.out_f32) launch_body<D, I8, true>(a, s);
-  else launch_body<D, I8, false>(a, s);
+  if (a.many_wgs) {
+    using Body = Q8Body<D, I8, 4, 4, 2>;
+    hipLaunchKernelGGL((decode_many_kernel<Body>), dim3(a.many_wgs), dim3(Body::kWaves * kWave), 0, s, a);
+  } else {
+    using Body = std::conditional_t<D == 64, Q8Body<D, I8, 6, 2, 4>, Q8Body<D, I8, 4, 4, 2>>;
+    hipLaunchKernelGGL((decode_ws_kernel<Body>), dim3(2 * a.ws_cu), dim3(Body::kWaves * kWave), 0, s, a);
+  }
 }
 
 }  // namespace

@@ -12,7 +12,7 @@
 // consecutive bytes of each of 16 K rows a load, and 64 consecutive V tiles,
 // of which each gives its lane four dimensions' codes of four tokens.  Codes of
 // either format are exact in bf16, and a power-of-two scale multiplies a score or a
-// probability without rounding it, so only sums and probabilities are rounded.
+// probability without rounding it, so only probabilities and sums are rounded, to fp32.
 #pragma once
 #include "aoh_device.h"
 
@@ -36,12 +36,6 @@ __device__ __forceinline__ float scale_of(uint32_t w) {
   else
     asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "s"(sh), "v"(w));
   return __builtin_bit_cast(float, r);
-}
-
-// Two floats rounded to bf16, the first in the low half.
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
 // Offset of the V code of dimension d, row r in its unit.
