@@ -313,10 +313,13 @@ aoh_status aoh_decode_step_noalloc(const aoh_tensor* q, const aoh_tensor* k_new,
  *            (c = 448 for AOH_E4M3, 127 for AOH_I8),
  *   code_d = x_d 2^-E rounded to the nearest code, ties to even,
  *   value_d = code_d 2^E,   scale byte = E + 127.
- * x_d 2^-E is exact, so the stored bits depend on the row alone.  A value is off
- * by at most 2^(E-1) < amax / 127 (AOH_I8), or by 2^-4 |x_d| and for
- * |x_d| < 2^(E-6) by 2^(E-10) (AOH_E4M3).  A row that holds a NaN, an infinity or
- * a magnitude of 2^127 or more is kept as NaN: scale byte 255, codes 0.
+ * x_d 2^-E is exact in fp32 unless it falls below fp32's normal range, where the
+ * code is 0 anyway, so the stored bits depend on the row alone.  A value is off by
+ * at most 2^(E-1) (AOH_I8), or by 2^-4 |x_d| and for |x_d| < 2^(E-6) by 2^(E-10)
+ * (AOH_E4M3).  Where E > -100, 2^(E-1) < amax / 127.  At E = -100, the least
+ * scale, the absolute bounds 2^-101 (AOH_I8) and 2^-110 (AOH_E4M3, |x_d| < 2^-106)
+ * remain, so rows of smaller values become zeros.  A row that holds a NaN, an
+ * infinity or a magnitude of 2^127 or more is kept as NaN: scale byte 255, codes 0.
  * AOH_E4M3 is the OCP fp8 format of that name (no infinities), AOH_I8 two's
  * complement.  Both caches of a call have one format.
  */
