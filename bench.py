@@ -123,12 +123,12 @@ def copy_calibration():
 PREFILL_SOURCES = ("prefill.hip", "aoh_device.h", "aoh_internal.h")
 DECODE_SOURCES = ("decode.hip", "decode_split.h", "aoh_device.h", "aoh_internal.h")
 TRAFFIC = {
-    "fetch_factor": 524299.7 / 1048576.0,   # FETCH_SIZE of a 1 GiB copy / 1 GiB
+    "fetch_factor": 524302.6 / 1048576.0,   # FETCH_SIZE of a 1 GiB copy / 1 GiB
     "write_factor": 1048576.0 / 1048576.0,  # WRITE_SIZE of a 1 GiB copy / 1 GiB
-    "prefill_mixed": {"fetch_kib": 465775.0, "write_kib": 263396.3,
-                      "sources": PREFILL_SOURCES, "source_hash": "f5ebfbb1542746d2"},
-    "decode_ws": {"fetch_kib": 1082956.1, "write_kib": 1169.8,
-                  "sources": DECODE_SOURCES, "source_hash": "f7e8359f719e01bf"},
+    "prefill_mixed": {"fetch_kib": 460987.5, "write_kib": 263391.5,
+                      "sources": PREFILL_SOURCES, "source_hash": "4fd65611b2099b8e"},
+    "decode_ws": {"fetch_kib": 1083440.1, "write_kib": 1169.8,
+                  "sources": DECODE_SOURCES, "source_hash": "be069d6ba15c221d"},
 }
 
 

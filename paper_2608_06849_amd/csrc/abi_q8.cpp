@@ -57,7 +57,7 @@ aoh_status fill_args(const aoh_paged_cache_q8* full, const aoh_ring_cache_q8* ri
   HeadSchedule hs;
   if ((st = schedule_heads(head_is_streaming, (int)std::min<int64_t>(Hkv, kMaxKvHeads + 1), &hs))) return st;
   if ((st = check_caches(full, ring, hs, n_sink, window, B, format))) return st;
-  a->B = (int)B; a->n = (int)n; a->Hkv = (int)Hkv;
+  a->B = (int)B; a->n = (int)n;
   if (hs.n_ret) {
     a->pk = static_cast<uint8_t*>(full->k); a->pv = static_cast<uint8_t*>(full->v); a->ps = full->scales;
     a->block_table = full->block_table;

@@ -193,7 +193,7 @@ struct Q8Args {
   const int32_t* cu_seqlens;    // writing packed tokens: device [B + 1]
   const int32_t* lens;          // reading: device [B]
   int32_t total;                // packed rows
-  int32_t B, n, Hkv;            // n: tokens of a sequence, at most
+  int32_t B, n;                 // n: tokens of a sequence, at most
   uint8_t* pk;                  // paged cache
   uint8_t* pv;
   uint8_t* ps;
