@@ -97,15 +97,21 @@ size_t decode_need(int64_t batch, int64_t hq, int64_t d) {
 // later (its tables) and merges the workgroups of an item one after the other, but
 // holds whole items, so it saves partials (of all query heads) at every item.  us a
 // step, work-space pass / many, half of the heads streaming, window 512, 300-6000 tokens
-// a sequence, then 2000-30000.  Width 128, 64 items of four heads 18.1 / 23.0, 37.6 / 43.0,
-// 128 of four 27.9 / 26.9, 63.5 / 63.8, of seven 33.0 / 27.7, 68.4 / 65.1, 256 of one
-// 35.8 / 36.6, 104.9 / 105.8, of two 39.0 / 36.8, 108.2 / 105.2, 32 of sixteen 22.1 / 33.8,
-// 41.5 / 56.7.  Width 64, 128 of four 17.7 / 18.5, 37.6 / 38.9, 256 of one 22.6 / 23.9,
-// 60.0 / 60.4, of four 27.2 / 24.5, 64.7 / 60.3, of two 24.2 / 24.1, 61.6 / 60.0.
+// a sequence, then 2000-30000.  Width 128, 64 items of four heads 16.8 / 23.1, 33.3 / 40.9,
+// 128 of four 25.2 / 24.4, 58.1 / 58.3, of seven 29.9 / 25.5, 62.9 / 60.1, 256 of one
+// 31.8 / 33.2, 97.5 / 98.3, of two 35.2 / 33.2, 101.0 / 98.4, 32 of sixteen 18.4 / 27.4,
+// 27.7 / 58.4.  Width 64, 128 of four 16.9 / 17.8, 33.3 / 34.9, 256 of one 20.7 / 22.4,
+// 54.2 / 53.8, of four 25.3 / 22.8, 58.4 / 54.2, of two 22.2 / 22.3, 55.9 / 54.8.
 // In caches of 32 blocks and fewer no item is in many workgroups (200-400 tokens,
-// window 256).  Width 128, 64 items of four heads 11.6 / 12.3, of seven 14.1 / 12.7, 60 of eight
-// 14.7 / 12.9, 32 of sixteen 14.9 / 15.1, 128 of four 17.3 / 13.2; width 64, 64 of seven
-// 10.6 / 11.0, 60 of sixteen 13.9 / 11.2, 128 of four 11.8 / 10.7.
+// window 256).  Width 128, 64 items of four heads 12.1 / 13.0, of seven 14.6 / 13.3, 60 of
+// eight 15.3 / 13.2, 32 of sixteen 15.5 / 16.4, 128 of four 17.7 / 13.5; width 64, 64 of
+// seven 11.3 / 11.9, 60 of sixteen 14.6 / 12.1, 128 of four 12.2 / 11.3.
+// The host knows the capacity only, not the lengths: short sequences in wide block
+// tables are judged as long ones (64 of 100-1000 tokens, two KV heads of width 64, 32
+// query heads: 22.7 here, 15.2 with many), and one long sequence among short ones, whose
+// many partials the other pass merges one after the other, loses where few KV heads
+// share it (64 sequences, one of 100000 tokens and 63 of 100-1000, two KV heads of
+// width 128, 32 query heads: 46.8 / 114.2; eight KV heads: 78.0 / 67.9).
 bool takes_many(int64_t B, int64_t Hkv, int gs, int D, int64_t blocks) {
   if (B > kWsMaxBatch) return true;
   const int64_t items = B * Hkv;

@@ -14,13 +14,13 @@
 // (width 64, int8) 51.7 / 53.1 / 56.0; the error of a bf16 output against float64,
 // relative to its norm, 1.68e-3 / 1.66e-3 / 1.66e-3 for the first of these, 1.89e-3 /
 // 1.62e-3 / 1.62e-3 for the last, and up to a quarter less in steps of few tokens.
-//   Bound: HBM.  8 sequences of 131072 tokens, 4 of 8 heads streaming, e4m3: 175 us
-// in the pass (1.09 GB of codes and scales, 1.03 times that fetched), 6.2 TB/s;
-// with an exponential only for every fourth score, or without converting codes, not
-// 1% less.  Width 64, whose pieces of memory are half as long: 5.4 TB/s.  Short
-// steps: a chain of memory latencies (lengths, block table, K, the join, the merge
-// launch).  The registers decide: with two chunks in flight the width 128 body
-// spilled, and the step above took 434 us.
+//   Bound: HBM.  8 sequences of 131072 tokens, 4 of 8 heads streaming, e4m3: 174-181
+// us in the pass (1.09 GB of codes and scales, 1.03 times that fetched), 6.0-6.3 TB/s;
+// a step with an exponential only for every fourth score 180.0 us, with all 179.7.
+// Width 64, whose pieces of memory are half as long: 5.6-5.9 TB/s over a step of 16
+// such sequences.  Short steps: a chain of memory latencies (lengths, block table, K,
+// the join, the merge launch).  The registers decide: with two chunks in flight the
+// width 128 body spilled, and the step above took 434 us.
 //   Lane group G = lane / 16 receives the scores of rows 4G .. 4G + 3 of a block,
 // and the k index of the second product is ordered so that it needs just those: P^T
 // stays in its lanes, and the V operand of dimension block 4j + n is word n of two
@@ -88,10 +88,12 @@ struct Q8Body {
   static constexpr bool kScores = false;
   static constexpr int kWaves = WAVES;
   static constexpr int kPerSimd = PER_SIMD;
-  // 300 sequences of up to 900 tokens: 56 us (63 with 4, 57 with 12); 96 of 200-8000: 100 (102, 101).
+  // 300 sequences of up to 900 tokens (width 64, int8): 56.6 us (63.8 with 4, 57.5 with 12); 96 of 200-8000: 82.7
+  // (83.0, 85.0).
   static constexpr int kItemCost = 8;
   // Work-space pass, where a segment is the whole workgroup's: 8 heads of width 128, sequences of 1 and
-  // 9532 tokens: 42.4 us with 0, 19.9 with 8, 17.5 with 16, 17.9 with 32.
+  // 9532 tokens: 35.9 us with 0, 14.4 with 8, 14.2 with 16, 14.5 with 32; 16 heads of which 9 stream, of 58 and
+  // 80104: 55.1, 33.7, 32.6, 33.0.
   static constexpr int kWsItemCost = 16;
   static constexpr int kBlocks = BLOCKS;
   static __device__ __forceinline__ int dim(int t, int G) { return 64 * (t >> 2) + 16 * G + 4 * (t & 3); }
@@ -341,11 +343,13 @@ namespace {
 
 // Waves of a workgroup, blocks of a chunk and waves of a SIMD (registers).  Width
 // 128: chunks of 16 KB in 250 registers, two workgroups of four waves a CU.  Width
-// 64, work-space pass: two of six waves with chunks of 4 KB (16 x 131072 tokens, 4 of
-// 8 heads streaming, e4m3: 202 us; 220 with four waves and 8 KB, 218 with eight and
-// 4 KB, 236 with four and 4 KB).  The pass for many items keeps four waves, since
-// more of them cut the items further (300 sequences of up to 900 tokens: 57 us, 87
-// with six waves).
+// 64, work-space pass: two of six waves with chunks of 4 KB, which suits short steps
+// (one sequence of 4093 tokens 8.8 us; 9.3 with four waves and 8 KB, 8.9 with eight
+// and 4 KB; 8 of 300-2000, int8, 10.4, 11.5 and 10.5) and is 1-8% behind in long ones
+// (16 of 131072, 4 of 8 heads streaming, e4m3 / int8: 187 / 197 us, 183 / 185, 181 / 187,
+// and 229 with four waves and 4 KB; 16 of 2000-32000, int8, 40.0, 38.1 and 37.0).  The
+// pass for many items keeps four waves, since more of them cut the items further (300
+// sequences of up to 900 tokens, int8: 56.6 us, 82.5 with six waves).
 template <int D, bool I8>
 void launch_format(const DecodeArgs& a, hipStream_t s) {
   if (a.many_wgs) {
