@@ -305,6 +305,85 @@ aoh_status aoh_decode_step_noalloc(const aoh_tensor* q, const aoh_tensor* k_new,
                                    int32_t window, aoh_tensor* out, void* stream);
 
 /*
+ * ------------------------------------------------- head norms and positions
+ * What a layer does between its projections and the calls above: the root mean
+ * square norm of each query and key head, and the rotation of pairs of its
+ * values by the token's position.  For a row x of D values
+ *   y_d = x_d / sqrt(mean_d(x_d^2) + eps) w_d    (with a weight w; else y = x)
+ *   pair i of the first n_pairs: (y_a, y_b) -> (y_a c - y_b s, y_b c + y_a s),
+ *     c = scale cos(p inv_freq[i]), s = scale sin(p inv_freq[i]),
+ *     (a, b) = (i, i + n_pairs), or with interleaved = 1 (2 i, 2 i + 1);
+ *   the values behind the first 2 n_pairs stay y.
+ * All of it in fp32 (the angle in fp64, so that far positions lose nothing),
+ * rounded once to the rows' dtype.
+ * p is the token's position on the axis of the pair: with one axis (n_axes = 1,
+ * axis NULL or zeros) and without a positions array its place in its sequence,
+ * start_pos[b] + t; else positions[axis[i]][token], any int32.  Several axes
+ * serve tokens of images and video (time, height, width).
+ */
+typedef struct {
+  const float* inv_freq; /* DEVICE fp32 [n_pairs], radians per position */
+  const uint8_t* axis;   /* HOST [n_pairs], each < n_axes; NULL: 0 */
+  int32_t n_pairs;       /* 1 <= n_pairs <= D/2 */
+  int32_t n_axes;        /* 1 .. 4 */
+  int32_t interleaved;   /* 0: pair (i, i + n_pairs); 1: (2 i, 2 i + 1) */
+  float scale;           /* factor of cosine and sine, 1 usually */
+} aoh_rope;
+
+/*
+ * Norm and rotation of the queries and keys of a prompt or chunk, one pass:
+ *   q, q_out: [B][T][Hq][D]; k, k_out: [B][T][Hkv][D], bf16 or fp32, one dtype.
+ *   q and q_out, or k and k_out, may be NULL (both of the pair).  An output may
+ *   be its input (same pointer and strides); otherwise outputs overlap nothing.
+ *   q_norm, k_norm: [D] weights, the rows' dtype or fp32 (one dtype for both);
+ *   NULL: that norm is left out.  eps >= 0.
+ *   rope: NULL for the norms alone; at least one of rope and the norms is given.
+ *   positions: DEVICE int32 [n_axes][B][T], contiguous, or NULL.
+ *   start_pos: DEVICE int32 [B] or NULL (0); used where positions is NULL.
+ * Packed tokens go through as one sequence [1][total] with their positions.
+ * B T <= 2^27.
+ */
+aoh_status aoh_qk_rope(const aoh_tensor* q, const aoh_tensor* k, const aoh_tensor* q_norm,
+                       const aoh_tensor* k_norm, float eps, const aoh_rope* rope,
+                       const int32_t* positions, const int32_t* start_pos, aoh_tensor* q_out,
+                       aoh_tensor* k_out, void* stream);
+
+/*
+ * The same for new tokens whose keys and values go into the caches: q_out, and
+ * caches as aoh_kv_append leaves them for the normed and rotated keys (bit for
+ * bit what aoh_qk_rope and aoh_kv_append give), in one launch and without a
+ * buffer for the keys.  Token t of sequence b goes to cache position
+ * start_pos[b] + t whatever `positions` holds.
+ *   q, q_out: [B][n_new][Hq][D] (both or neither NULL); k_new, v_new:
+ *   [B][n_new][Hkv][D]; q_out may be q.  rope, norms, eps, positions
+ *   ([n_axes][B][n_new]) as above; here all of them may be left out.
+ *   start_pos: DEVICE int32 [B] or NULL (0).  A sequence whose start_pos is
+ *   negative or above 2^30 is left out: nothing of it is written, q_out included.
+ * Token-major V pages are accepted.  n_new <= 2^26, B n_new < 2^31.
+ */
+aoh_status aoh_kv_append_rope(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
+                              const aoh_tensor* q_norm, const aoh_tensor* k_norm, float eps,
+                              const aoh_rope* rope, const int32_t* positions,
+                              const uint8_t* head_is_streaming, const int32_t* start_pos,
+                              const aoh_paged_cache* kv_full, const aoh_ring_cache* kv_ring,
+                              int32_t n_sink, int32_t window, aoh_tensor* q_out, void* stream);
+
+/*
+ * The same for packed tokens: q, q_out [total][Hq][D], k_new, v_new
+ * [total][Hkv][D]; sequence b's tokens are rows cu_seqlens[b] ..
+ * cu_seqlens[b+1] - 1 (DEVICE int32 [batch + 1], ascending; rows outside the
+ * tensors and beyond max_new of a sequence are left out, as are rows behind the
+ * last sequence).  positions: [n_axes][total].
+ */
+aoh_status aoh_kv_append_rope_varlen(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
+                                     const int32_t* cu_seqlens, int32_t batch, int32_t max_new,
+                                     const aoh_tensor* q_norm, const aoh_tensor* k_norm, float eps,
+                                     const aoh_rope* rope, const int32_t* positions,
+                                     const uint8_t* head_is_streaming, const int32_t* start_pos,
+                                     const aoh_paged_cache* kv_full, const aoh_ring_cache* kv_ring,
+                                     int32_t n_sink, int32_t window, aoh_tensor* q_out, void* stream);
+
+/*
  * ------------------------------------------------------------ 8-bit caches
  * The two caches with K and V in 8 bits: half the resident bytes, and half of
  * what a decode step reads.  Every row (one token, one KV head, K or V) has one

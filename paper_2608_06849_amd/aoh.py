@@ -49,6 +49,11 @@ class AohRingCache(ctypes.Structure):
                 ("capacity", ctypes.c_int32), ("batch", ctypes.c_int32)]
 
 
+class AohRope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("n_pairs", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class AohPagedCacheQ8(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("block_table", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
@@ -66,6 +71,7 @@ _lib = None
 
 EXPORTS = ("aoh_prefill", "aoh_prefill_chunked", "aoh_prefill_append", "aoh_prefill_varlen", "aoh_kv_append", "aoh_decode_workspace_bytes", "aoh_decode", "aoh_decode_step",
            "aoh_decode_step_noalloc",
+           "aoh_qk_rope", "aoh_kv_append_rope", "aoh_kv_append_rope_varlen",
            "aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8_workspace_bytes",
            "aoh_decode_q8", "aoh_decode_step_q8",
            "aoh_classify_workspace_bytes", "aoh_classify", "aoh_retrieval_group_count",
@@ -136,11 +142,23 @@ def lib():
         L.aoh_decode_q8.restype = ctypes.c_int
         L.aoh_decode_step_q8.argtypes = [P(AohTensor)] * 3 + L.aoh_decode_q8.argtypes[1:]
         L.aoh_decode_step_q8.restype = ctypes.c_int
+        rope = [P(AohTensor)] * 2 + [ctypes.c_float, P(AohRope), ctypes.c_void_p]  # norms, rotation, positions
+        caches = [P(AohPagedCache), P(AohRingCache), ctypes.c_int32, ctypes.c_int32]
+        L.aoh_qk_rope.argtypes = [P(AohTensor)] * 2 + rope + [ctypes.c_void_p] + [P(AohTensor)] * 2 + [ctypes.c_void_p]
+        L.aoh_qk_rope.restype = ctypes.c_int
+        L.aoh_kv_append_rope.argtypes = [P(AohTensor)] * 3 + rope + [ctypes.c_void_p] * 2 + caches + [P(AohTensor),
+                                                                                                  ctypes.c_void_p]
+        L.aoh_kv_append_rope.restype = ctypes.c_int
+        L.aoh_kv_append_rope_varlen.argtypes = [P(AohTensor)] * 3 + [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32] + \
+            L.aoh_kv_append_rope.argtypes[3:]
+        L.aoh_kv_append_rope_varlen.restype = ctypes.c_int
         # The same entry points with descriptors as packed bytes (_q8_desc): 0.7 us each less on the host.
         L.packed = {}
-        for name in ("aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8", "aoh_decode_step_q8"):
+        for name in ("aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8", "aoh_decode_step_q8",
+                     "aoh_qk_rope", "aoh_kv_append_rope", "aoh_kv_append_rope_varlen"):
             f = L.packed[name] = L[name]
-            f.argtypes = [ctypes.c_char_p if t is P(AohTensor) else t for t in getattr(L, name).argtypes]
+            f.argtypes = [ctypes.c_char_p if t in (P(AohTensor), P(AohPagedCache), P(AohRingCache)) else t
+                          for t in getattr(L, name).argtypes]
             f.restype = ctypes.c_int
         L.aoh_classify_workspace_bytes.argtypes = [ctypes.c_int32] * 4
         L.aoh_classify_workspace_bytes.restype = ctypes.c_size_t
@@ -644,6 +662,152 @@ def aoh_decode_step_q8(q, k_new, v_new, kv_full, kv_ring, head_is_streaming, len
     call: the same result and caches as aoh_kv_append_q8 + aoh_decode_q8."""
     return _decode_q8("aoh_decode_step_q8", (k_new, v_new), q, kv_full, kv_ring, head_is_streaming, lens, n_sink,
                       window, out, workspace, stream)
+
+
+# ----------------------------------------------------------------------------- head norms and positions
+
+class Rope(_Fixed):
+    """A position rotation: frequencies inv_freq [pairs] (fp32, on the GPU; radians per position) of the first
+    2 * pairs values of a head, which pair up as (i, i + pairs), or with interleaved (2 i, 2 i + 1); scale multiplies
+    cosine and sine.  axis: for each pair the row of the positions that turns it (several axes), or None."""
+
+    def __init__(self, inv_freq, axis=None, interleaved=False, scale=1.0):
+        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous fp32 vector")
+        pairs = inv_freq.shape[0]
+        axis = None if axis is None else bytes(map(int, axis))
+        if axis is not None and len(axis) != pairs:
+            raise ValueError(f"{len(axis)} axes given for {pairs} pairs")
+        self.inv_freq, self.axis, self.interleaved, self.scale = inv_freq, axis, bool(interleaved), float(scale)
+        self.n_axes = 1 + max(axis, default=0) if axis else 1
+        self.device = inv_freq.device
+        self._axis = ctypes.create_string_buffer(axis, max(pairs, 1)) if axis is not None else None
+        self._desc = AohRope(inv_freq.data_ptr(), ctypes.cast(self._axis, ctypes.c_void_p) if axis is not None else None,
+                             pairs, self.n_axes, int(self.interleaved), self.scale)
+        self._ref = ctypes.byref(self._desc)
+
+
+def _desc(t, name, device, width):
+    """aoh_tensor descriptor, as bytes, of a tensor that has to be on `device`, with rows of `width`."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    shape = t.shape
+    n = len(shape)
+    if n not in _PACK or shape[-1] != width:
+        raise ValueError(f"{name}: shape {tuple(shape)}, for rows of width {width}")
+    return _PACK[n](t.data_ptr(), dtype, n, *shape, *t.stride())
+
+
+_PACK_PAGED, _PACK_RING = struct.Struct("@PPPqiiii").pack, struct.Struct("@PPiii4x").pack
+
+
+def _cache_descs(kv_full, kv_ring, device, width, dtype):
+    """Descriptors of the caches, as bytes; their tensors have to be contiguous, of `dtype` and on `device`."""
+    full = ring = None
+    for c, name in ((kv_full, "kv_full"), (kv_ring, "kv_ring")):
+        if c is None:
+            continue
+        for t in (c.k, c.v):
+            if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() != c.k.numel():
+                raise ValueError(f"{name} must be contiguous {dtype} tensors of one size on {device}")
+        if c.k.shape[-1] != width:
+            raise ValueError(f"{name} has rows of width {c.k.shape[-1]}, not {width}")
+    if kv_full is not None:
+        table = kv_full.block_table
+        _check_i32(table, "block_table", device)
+        k = kv_full.k.shape
+        rows, cols = table.shape
+        full = _PACK_PAGED(kv_full.k.data_ptr(), kv_full.v.data_ptr(), table.data_ptr(), k[0], cols, k[1], rows,
+                           kv_full.v_token_major)
+    if kv_ring is not None:
+        k, cap = kv_ring.k.shape, kv_ring.capacity
+        if k[2] * PAGE_TOKENS < cap:
+            raise ValueError(f"kv_ring has {k[2]} blocks for a capacity of {cap}")
+        ring = _PACK_RING(kv_ring.k.data_ptr(), kv_ring.v.data_ptr(), k[1], cap, k[0])
+    return full, ring
+
+
+def _rope_args(rope, q_norm, k_norm, eps, positions, tokens, device, width):
+    """Norms, rotation and positions of a call over that many tokens."""
+    if rope is not None and rope.device != device:
+        raise ValueError(f"the rotation is on {rope.device}, not on {device}")
+    if positions is not None:
+        _check_i32(positions, "positions", device)
+        n = rope.n_axes if rope is not None else 1
+        if positions.numel() != n * tokens:
+            raise ValueError(f"positions has {positions.numel()} entries for {n} axes of {tokens} tokens")
+    return (_desc(q_norm, "q_norm", device, width) if q_norm is not None else None,
+            _desc(k_norm, "k_norm", device, width) if k_norm is not None else None, eps,
+            rope._ref if rope is not None else None, positions.data_ptr() if positions is not None else None)
+
+
+def _on_gpu(t, name):
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} is on {t.device}")
+    return t.device
+
+
+def aoh_qk_rope(q, k, rope, q_norm=None, k_norm=None, eps=1e-6, positions=None, start_pos=None, q_out=None, k_out=None,
+                stream=None):
+    """Norm (weights q_norm, k_norm [D]) and rotation of q [B,T,Hq,D] and k [B,T,Hkv,D]; either may be None, and so may
+    rope or the norms.  positions: int32 [axes, B, T], or None: start_pos[b] + t.  q_out = q, k_out = k work in place.
+    Returns (q_out, k_out)."""
+    one = q if q is not None else k
+    if one is None:
+        raise ValueError("neither q nor k given")
+    dev, d = _on_gpu(one, "q" if q is not None else "k"), one.shape[-1]
+    # checked before an output is allocated
+    qd = _desc(q, "q", dev, d) if q is not None else None
+    kd = _desc(k, "k", dev, d) if k is not None else None
+    args = _rope_args(rope, q_norm, k_norm, eps, positions, one.shape[0] * one.shape[1] if one.dim() > 1 else 0, dev, d)
+    start = _q8_seqs(start_pos, "start_pos", dev, one.shape[0]) if start_pos is not None else None
+    if q is not None and q_out is None:
+        q_out = _result(stream, torch.empty_like, q)
+    if k is not None and k_out is None:
+        k_out = _result(stream, torch.empty_like, k)
+    _q8_run("aoh_qk_rope", dev, stream, qd, kd, *args, start, _desc(q_out, "q_out", dev, d) if q_out is not None else None,
+            _desc(k_out, "k_out", dev, d) if k_out is not None else None)
+    return q_out, k_out
+
+
+def _append_rope(call, q, k_new, v_new, lead, tokens, seqs, rope, head_is_streaming, start_pos, kv_full, kv_ring, n_sink,
+                 window, q_norm, k_norm, eps, positions, q_out, stream):
+    dev, d = _on_gpu(k_new, "k_new"), k_new.shape[-1]
+    qd = _desc(q, "q", dev, d) if q is not None else None
+    kd, vd = _desc(k_new, "k_new", dev, d), _desc(v_new, "v_new", dev, d)
+    args = _rope_args(rope, q_norm, k_norm, eps, positions, tokens, dev, d)
+    start = _q8_seqs(start_pos, "start_pos", dev, seqs) if start_pos is not None else None
+    m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
+    full, ring = _cache_descs(kv_full, kv_ring, dev, d, k_new.dtype)
+    if q is not None and q_out is None:
+        q_out = _result(stream, torch.empty_like, q)
+    _q8_run(call, dev, stream, qd, kd, vd, *lead, *args, m, start, full, ring, n_sink, window,
+            _desc(q_out, "q_out", dev, d) if q_out is not None else None)
+    return q_out
+
+
+def aoh_kv_append_rope(q, k_new, v_new, rope, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, q_norm=None,
+                       k_norm=None, eps=1e-6, positions=None, q_out=None, stream=None):
+    """Norm and rotate q [B,n_new,Hq,D] (None: no queries) and k_new [B,n_new,Hkv,D], and append the keys and v_new at
+    positions start_pos[b] + t (None: t): the same as aoh_qk_rope and aoh_kv_append.  positions [axes, B, n_new] turn the
+    rows where given, else the cache positions.  Returns q_out."""
+    n = k_new.shape[0] * k_new.shape[1] if k_new.dim() > 1 else 0
+    return _append_rope("aoh_kv_append_rope", q, k_new, v_new, (), n, k_new.shape[0], rope, head_is_streaming, start_pos,
+                        kv_full, kv_ring, n_sink, window, q_norm, k_norm, eps, positions, q_out, stream)
+
+
+def aoh_kv_append_rope_varlen(q, k_new, v_new, cu_seqlens, max_new, rope, head_is_streaming, start_pos, kv_full, kv_ring,
+                              n_sink, window, q_norm=None, k_norm=None, eps=1e-6, positions=None, q_out=None, stream=None):
+    """aoh_kv_append_rope of packed tokens [total,H,D]: sequence b's are rows cu_seqlens[b] .. cu_seqlens[b+1]-1, at most
+    max_new; positions [axes, total]."""
+    n = cu_seqlens.numel() - 1
+    cu = _q8_seqs(cu_seqlens, "cu_seqlens", k_new.device, 2) if n > 0 else None
+    return _append_rope("aoh_kv_append_rope_varlen", q, k_new, v_new, (cu, n, max_new), k_new.shape[0], n, rope,
+                        head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, q_norm, k_norm, eps, positions,
+                        q_out, stream)
 
 
 # ----------------------------------------------------------------------------- classifier

@@ -10,6 +10,7 @@ namespace aoh {
 
 constexpr int kMaxKvHeads = 64;
 constexpr int kPageTokens = 16;  // tokens per cache page / ring block
+constexpr int kMaxPairs = 64;    // rotated pairs of a head
 
 // One prefill launch covers every query head of the KV heads in kv_heads[]
 // (all of one type).  Work item = (batch, query head, query block).
@@ -214,6 +215,49 @@ struct Q8Args {
 hipError_t launch_q8(const Q8Args& a, int dtype, int format, int d, bool write, hipStream_t s);
 // Split pass of a decode step over the 8-bit caches (a.ws_cu, a.many_wgs as in launch_decode_split).
 hipError_t launch_decode_q8_split(const DecodeArgs& a, int d, int format, hipStream_t s);
+
+// Head norms and position rotation of queries and keys (rope.hip), with append: keys and
+// values into the caches.
+struct RopeArgs {
+  const void* q;                // [B][T][H][D], or packed [total][H][D] (cu_seqlens; *_sb = 0)
+  const void* k;
+  const void* v;
+  void* q_out;
+  void* k_out;                  // without append
+  int64_t q_sb, q_st, q_sh;
+  int64_t k_sb, k_st, k_sh;
+  int64_t v_sb, v_st, v_sh;
+  int64_t qo_sb, qo_st, qo_sh;
+  int64_t ko_sb, ko_st, ko_sh;
+  const void* q_norm;           // [D] weights; nullptr: no norm
+  const void* k_norm;
+  int32_t norm_f32;             // the weights are fp32 (else of the rows' dtype)
+  float eps;
+  const float* inv_freq;        // [n_pairs]
+  int32_t n_pairs;              // 0: no rotation
+  int32_t interleaved;
+  float scale;
+  const int32_t* positions;     // [axes][pos_stride]; nullptr: start_pos[b] + t
+  int64_t pos_stride;
+  const int32_t* start_pos;     // [B]; nullptr: 0
+  const int32_t* cu_seqlens;    // [B + 1], packed appends
+  int32_t total;                // packed rows
+  int32_t B, T;                 // T: tokens of a sequence, at most
+  int32_t Hq, Hkv;              // 0: no queries / no keys
+  int32_t heads_per_wg;         // set by the launcher
+  // caches (append), as in AppendArgs
+  void* pk;
+  void* pv;
+  const int32_t* block_table;
+  int32_t max_pages, num_pages, n_ret, v_token_major;
+  void* rk;
+  void* rv;
+  int32_t n_str, ring_blocks, n_sink, window;
+  uint64_t streaming_mask;
+  uint8_t rank[kMaxKvHeads];
+  uint8_t axis[kMaxPairs];      // axis of each pair
+};
+hipError_t launch_rope(const RopeArgs& a, int dtype, int d, bool append, hipStream_t s);
 
 // The head classifier over L layers.  Weights are bf16 [L][H * D][d_model]
 // slices (layer stride *_sl, row stride *_sr, unit column stride).
