@@ -384,6 +384,60 @@ aoh_status aoh_kv_append_rope_varlen(const aoh_tensor* q, const aoh_tensor* k_ne
                                      int32_t n_sink, int32_t window, aoh_tensor* q_out, void* stream);
 
 /*
+ * ------------------------------------------------------------ running prompts
+ * Attention of several new tokens of each sequence over what the caches hold of
+ * it and over themselves: the next chunk of a prompt (Sec. 5, chunked-prefill
+ * stage), the next message of a conversation, drafted tokens to verify.
+ * Query t of sequence b stands at position p = start_pos[b] + t; its keys are
+ * the cached positions j < start_pos[b] and the new tokens up to t.
+ *   retrieval heads: all of them;
+ *   streaming heads, evict = 0: j < n_sink or p - j < window, as aoh_prefill and
+ *     decode (whatever the cuts, a prompt taken in chunks gives the rows of
+ *     aoh_prefill); evict = 1: j < n_sink or j >= start_pos[b] - window, the
+ *     cache as it was before the chunk (a prompt taken in chunks of K tokens
+ *     gives the rows of aoh_prefill_chunked with K).
+ *   out[b,t,h,:] = sum_j softmax_j(q[b,t,h,:] . k_j / sqrt(D)) v_j
+ *   q: [B][n_new][Hq][D]; k_new, v_new: [B][n_new][Hkv][D]; out: [B][n_new][Hq][D],
+ *     dtype of q, or fp32 for bf16 q (the weights then stay whole before the
+ *     product with V, where a bf16 output takes them rounded to bf16).
+ *   start_pos: DEVICE int32 [B] or NULL (0): the tokens that the caches hold.
+ *     Positions beyond the block table and pages outside [0, num_pages) are not
+ *     seen.  A sequence whose start_pos is negative or above 2^30 is left out:
+ *     its rows of out stay as they were, its cache too.
+ *   append = 1: after the attention, on the same stream, the new tokens go into
+ *     the caches as aoh_kv_append writes them.  The call reads the caches before
+ *     that, so append = 0 and an aoh_kv_append later (of the tokens that are kept)
+ *     give the same.
+ *   workspace: DEVICE, aoh_extend_workspace_bytes(...) bytes, 16-byte aligned
+ *     (fp32: none needed); calls that share one must not overlap.
+ * What a query does not see has no influence, whatever its bits: keys beyond it,
+ * rows behind a sequence's end, slots and pages without a token.
+ * Dimension-major V pages only; Hq / Hkv <= 16; n_new <= 2^26, B n_new < 2^31.
+ * Grids depend on shapes only (start_pos is read on the device), so calls can be
+ * captured in HIP graphs.
+ */
+size_t aoh_extend_workspace_bytes(int32_t batch, int32_t max_new, int32_t n_q_heads, int32_t n_kv_heads,
+                                  int32_t d_head);
+aoh_status aoh_extend(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
+                      const uint8_t* head_is_streaming, const int32_t* start_pos,
+                      const aoh_paged_cache* kv_full, const aoh_ring_cache* kv_ring, int32_t n_sink,
+                      int32_t window, int32_t evict, int32_t append, aoh_tensor* out, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * The same for packed tokens: q, out [total][Hq][D], k_new, v_new [total][Hkv][D];
+ * sequence b's tokens are rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (DEVICE int32
+ * [batch + 1], ascending), at most max_new of them; a sequence may have none.
+ * Rows behind the last sequence stay as they were.
+ */
+aoh_status aoh_extend_varlen(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
+                             const int32_t* cu_seqlens, int32_t batch, int32_t max_new,
+                             const uint8_t* head_is_streaming, const int32_t* start_pos,
+                             const aoh_paged_cache* kv_full, const aoh_ring_cache* kv_ring, int32_t n_sink,
+                             int32_t window, int32_t evict, int32_t append, aoh_tensor* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * ------------------------------------------------------------ 8-bit caches
  * The two caches with K and V in 8 bits: half the resident bytes, and half of
  * what a decode step reads.  Every row (one token, one KV head, K or V) has one

@@ -72,6 +72,7 @@ _lib = None
 EXPORTS = ("aoh_prefill", "aoh_prefill_chunked", "aoh_prefill_append", "aoh_prefill_varlen", "aoh_kv_append", "aoh_decode_workspace_bytes", "aoh_decode", "aoh_decode_step",
            "aoh_decode_step_noalloc",
            "aoh_qk_rope", "aoh_kv_append_rope", "aoh_kv_append_rope_varlen",
+           "aoh_extend_workspace_bytes", "aoh_extend", "aoh_extend_varlen",
            "aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8_workspace_bytes",
            "aoh_decode_q8", "aoh_decode_step_q8",
            "aoh_classify_workspace_bytes", "aoh_classify", "aoh_retrieval_group_count",
@@ -152,10 +153,18 @@ def lib():
         L.aoh_kv_append_rope_varlen.argtypes = [P(AohTensor)] * 3 + [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32] + \
             L.aoh_kv_append_rope.argtypes[3:]
         L.aoh_kv_append_rope_varlen.restype = ctypes.c_int
+        L.aoh_extend_workspace_bytes.argtypes = [ctypes.c_int32] * 5
+        L.aoh_extend_workspace_bytes.restype = ctypes.c_size_t
+        L.aoh_extend.argtypes = [P(AohTensor)] * 3 + [ctypes.c_void_p] * 2 + caches + \
+            [ctypes.c_int32, ctypes.c_int32, P(AohTensor), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        L.aoh_extend.restype = ctypes.c_int
+        L.aoh_extend_varlen.argtypes = [P(AohTensor)] * 3 + [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32] + \
+            L.aoh_extend.argtypes[3:]
+        L.aoh_extend_varlen.restype = ctypes.c_int
         # The same entry points with descriptors as packed bytes (_q8_desc): 0.7 us each less on the host.
         L.packed = {}
         for name in ("aoh_kv_append_q8", "aoh_kv_append_q8_varlen", "aoh_kv_read_q8", "aoh_decode_q8", "aoh_decode_step_q8",
-                     "aoh_qk_rope", "aoh_kv_append_rope", "aoh_kv_append_rope_varlen"):
+                     "aoh_qk_rope", "aoh_kv_append_rope", "aoh_kv_append_rope_varlen", "aoh_extend", "aoh_extend_varlen"):
             f = L.packed[name] = L[name]
             f.argtypes = [ctypes.c_char_p if t in (P(AohTensor), P(AohPagedCache), P(AohRingCache)) else t
                           for t in getattr(L, name).argtypes]
@@ -808,6 +817,52 @@ def aoh_kv_append_rope_varlen(q, k_new, v_new, cu_seqlens, max_new, rope, head_i
     return _append_rope("aoh_kv_append_rope_varlen", q, k_new, v_new, (cu, n, max_new), k_new.shape[0], n, rope,
                         head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, q_norm, k_norm, eps, positions,
                         q_out, stream)
+
+
+# ----------------------------------------------------------------------------- running prompts
+
+def aoh_extend_workspace_bytes(batch, max_new, n_q_heads, n_kv_heads, d_head):
+    return int(lib().aoh_extend_workspace_bytes(batch, max_new, n_q_heads, n_kv_heads, d_head))
+
+
+def _extend(call, q, k_new, v_new, lead, seqs, longest, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, evict,
+            append, out, workspace, stream):
+    dev, d = _on_gpu(q, "q"), q.shape[-1]
+    qd, kd, vd = _desc(q, "q", dev, d), _desc(k_new, "k_new", dev, d), _desc(v_new, "v_new", dev, d)
+    start = _q8_seqs(start_pos, "start_pos", dev, seqs) if start_pos is not None else None
+    m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
+    full, ring = _cache_descs(kv_full, kv_ring, dev, d, q.dtype)
+    if workspace is None:
+        n = aoh_extend_workspace_bytes(seqs, longest, q.shape[-2], k_new.shape[-2], d) if q.dim() > 1 and k_new.dim() > 1 else 0
+        workspace = _scratch(stream, torch.empty, n, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"the workspace must be contiguous and on {dev}")
+    if out is None:
+        out = _result(stream, torch.empty_like, q)
+    _q8_run(call, dev, stream, qd, kd, vd, *lead, m, start, full, ring, n_sink, window, int(evict), int(append),
+            _desc(out, "out", dev, d), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return out
+
+
+def aoh_extend(q, k_new, v_new, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, evict=False, append=True,
+               out=None, workspace=None, stream=None):
+    """Attention of new tokens q [B,n_new,Hq,D] at positions start_pos[b] + t (None: t) over the caches, which hold the
+    positions before them, and over themselves (k_new, v_new [B,n_new,Hkv,D]); then, with append, K and V go into the
+    caches.  evict: streaming heads see the cache as it was before the tokens (chunk eviction), else their per-token
+    window."""
+    b, n = (q.shape[0], q.shape[1]) if q.dim() > 1 else (1, 1)
+    return _extend("aoh_extend", q, k_new, v_new, (), b, n, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window,
+                   evict, append, out, workspace, stream)
+
+
+def aoh_extend_varlen(q, k_new, v_new, cu_seqlens, max_new, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window,
+                      evict=False, append=True, out=None, workspace=None, stream=None):
+    """aoh_extend of packed tokens [total,H,D]: sequence b's are rows cu_seqlens[b] .. cu_seqlens[b+1]-1, at most
+    max_new; rows behind the last sequence stay as they were."""
+    n = cu_seqlens.numel() - 1
+    cu = _q8_seqs(cu_seqlens, "cu_seqlens", q.device, 2) if n > 0 else None
+    return _extend("aoh_extend_varlen", q, k_new, v_new, (cu, n, max_new), n, max_new, head_is_streaming, start_pos, kv_full,
+                   kv_ring, n_sink, window, evict, append, out, workspace, stream)
 
 
 # ----------------------------------------------------------------------------- classifier

@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libaoh.so")
 SOURCES = ["abi.cpp", "prefill.hip", "decode.hip", "kv_append.hip", "classify.hip", "topk.hip", "noalloc.hip",
-           "abi_q8.cpp", "kv_q8.hip", "decode_q8.hip", "abi_rope.cpp", "rope.hip"]
+           "abi_q8.cpp", "kv_q8.hip", "decode_q8.hip", "abi_rope.cpp", "rope.hip",
+           "abi_extend.cpp", "extend.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 # Packed-fp32 VALU instructions are kept out of generated code on purpose.

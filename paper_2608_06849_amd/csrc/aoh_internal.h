@@ -259,6 +259,37 @@ struct RopeArgs {
 };
 hipError_t launch_rope(const RopeArgs& a, int dtype, int d, bool append, hipStream_t s);
 
+// Attention of new tokens over the caches and themselves (extend.hip).
+struct ExtendArgs {
+  const void* q;                // [B][T][H][D], or packed [total][H][D] (cu_seqlens; *_sb = 0)
+  const void* k;
+  const void* v;
+  void* out;
+  int64_t q_sb, q_st, q_sh;
+  int64_t k_sb, k_st, k_sh;
+  int64_t v_sb, v_st, v_sh;
+  int64_t o_sb, o_st, o_sh;
+  const int32_t* start_pos;     // [B]; nullptr: 0
+  const int32_t* cu_seqlens;    // [B + 1], packed
+  int32_t total;                // packed rows
+  int32_t B, T, Hq, gs;         // T: new tokens of a sequence, at most
+  int32_t n_sink, window, ring_cap;
+  int32_t evict;                // streaming mask: 0 per-token band, 1 the cache as it was before the tokens
+  int32_t out_f32;
+  float scale_log2, scale;
+  const void* pk;               // caches, as in AppendArgs
+  const void* pv;
+  const int32_t* block_table;
+  int32_t max_pages, num_pages, n_ret;
+  const void* rk;
+  const void* rv;
+  int32_t n_str, ring_blocks;
+  uint64_t streaming_mask;
+  uint8_t rank[kMaxKvHeads];
+  uint8_t kv_heads[kMaxKvHeads];  // retrieval heads, then streaming ones
+};
+hipError_t launch_extend(const ExtendArgs& a, int dtype, int d, hipStream_t s);
+
 // The head classifier over L layers.  Weights are bf16 [L][H * D][d_model]
 // slices (layer stride *_sl, row stride *_sr, unit column stride).
 struct ClassifyArgs {
