@@ -38,7 +38,7 @@ def put(**kw):
 
 
 CASES = [
-    (("dense",), put(q=None), INV, "q"), (("dense",), put(k=_t((2, 5, 2, 64))), INV, "width"), (("dense",), put(v=_t((2, 5, 1, 128))), INV, "shapes"),
+    (("dense",), put(q=None), INV, "q"), (("dense",), put(k=_t((2, 5, 2, 64)), v=_t((2, 5, 2, 64))), INV, "width"), (("dense",), put(v=_t((2, 5, 1, 128))), INV, "shapes"),
     (("dense",), put(k=_t((2, 6, 2, 128)), v=_t((2, 6, 2, 128))), INV, "tokens"), (("dense",), put(out=_t((2, 5, 4, 128))), INV, "out"),
     (("dense",), put(k=_t((2, 5, 2, 128), A.AOH_F32)), UNS, "k_new"),
     (("dense",), lambda c: [setattr(c, n, _t((2, 5, h, 128), A.AOH_F32)) for n, h in (("q", 8), ("k", 2), ("v", 2))], UNS, "out"),
