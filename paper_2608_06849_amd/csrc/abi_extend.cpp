@@ -53,6 +53,14 @@ aoh_status extend_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
     return fail(AOH_ERR_UNSUPPORTED, "aoh_extend needs dimension-major V pages (kv_full.v_token_major=0)");
   if ((st = check_ring(kv_ring, hs.n_str, n_sink, window, B))) return st;
 
+  const int cus = std::min(compute_units(), kWsMaxWgs / 2);
+  if (dt == AOH_BF16) {
+    const size_t need = extend_workspace((int)D, kWsMaxWgs / 2);
+    if (!workspace) return fail(AOH_ERR_WORKSPACE, "workspace is null; %zu bytes needed", need);
+    if (workspace_bytes < need) return fail(AOH_ERR_WORKSPACE, "workspace has %zu bytes; %zu needed", workspace_bytes, need);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(AOH_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  }
+
   ExtendArgs a;
   std::memset(&a, 0, sizeof(a));
   const int i = nd - 3;  // the token axis
@@ -84,6 +92,8 @@ aoh_status extend_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
   std::memcpy(a.rank, hs.rank, sizeof(a.rank));
   std::memcpy(a.kv_heads, hs.ret, hs.n_ret);
   std::memcpy(a.kv_heads + hs.n_ret, hs.str, hs.n_str);
+  a.workspace = workspace;
+  a.cus = cus;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = launch_extend(a, dt, (int)D, s);
   if (e != hipSuccess) return fail(AOH_ERR_HIP, "extend launch: %s", hipGetErrorString(e));
@@ -118,7 +128,7 @@ size_t aoh_extend_workspace_bytes(int32_t batch, int32_t max_new, int32_t n_q_he
   if (batch < 1 || max_new < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads ||
       n_q_heads / n_kv_heads > 16 || (d_head != 64 && d_head != 128))
     return 0;
-  return 16;
+  return extend_workspace(d_head, kWsMaxWgs / 2);
 }
 
 aoh_status aoh_extend(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,

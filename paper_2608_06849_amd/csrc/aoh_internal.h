@@ -287,7 +287,15 @@ struct ExtendArgs {
   uint64_t streaming_mask;
   uint8_t rank[kMaxKvHeads];
   uint8_t kv_heads[kMaxKvHeads];  // retrieval heads, then streaming ones
+  void* workspace;              // extend_workspace bytes (bf16)
+  int32_t cus;                  // compute units
+  // set by the launcher: workgroups, the fewest tiles of one, and the partials of two blocks
+  // of rows a workgroup, [2 wgs][rows][D] and (m in log2 units, l)
+  int32_t wgs, min_tiles;
+  float* part_acc;
+  float* part_ml;
 };
+size_t extend_workspace(int d, int cus);
 hipError_t launch_extend(const ExtendArgs& a, int dtype, int d, hipStream_t s);
 
 // The head classifier over L layers.  Weights are bf16 [L][H * D][d_model]
