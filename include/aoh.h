@@ -408,15 +408,16 @@ aoh_status aoh_kv_append_rope_varlen(const aoh_tensor* q, const aoh_tensor* k_ne
  *     the caches as aoh_kv_append writes them.  The call reads the caches before
  *     that, so append = 0 and an aoh_kv_append later (of the tokens that are kept)
  *     give the same.
- *   workspace: DEVICE, aoh_extend_workspace_bytes(...) bytes, 16-byte aligned
- *     (fp32: none needed); calls that share one must not overlap.
+ *   workspace: DEVICE, aoh_extend_workspace_bytes(...) bytes for B sequences of
+ *     n_tokens new tokens in all, 16-byte aligned (fp32: none needed); a size for
+ *     more sequences or tokens serves fewer.  Calls that share one must not overlap.
  * What a query does not see has no influence, whatever its bits: keys beyond it,
  * rows behind a sequence's end, slots and pages without a token.
  * Dimension-major V pages only; Hq / Hkv <= 16; n_new <= 2^26, B n_new < 2^31.
  * Grids depend on shapes only (start_pos is read on the device), so calls can be
  * captured in HIP graphs.
  */
-size_t aoh_extend_workspace_bytes(int32_t batch, int32_t max_new, int32_t n_q_heads, int32_t n_kv_heads,
+size_t aoh_extend_workspace_bytes(int32_t batch, int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
                                   int32_t d_head);
 aoh_status aoh_extend(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
                       const uint8_t* head_is_streaming, const int32_t* start_pos,

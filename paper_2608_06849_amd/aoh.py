@@ -153,7 +153,7 @@ def lib():
         L.aoh_kv_append_rope_varlen.argtypes = [P(AohTensor)] * 3 + [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32] + \
             L.aoh_kv_append_rope.argtypes[3:]
         L.aoh_kv_append_rope_varlen.restype = ctypes.c_int
-        L.aoh_extend_workspace_bytes.argtypes = [ctypes.c_int32] * 5
+        L.aoh_extend_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.c_int64] + [ctypes.c_int32] * 3
         L.aoh_extend_workspace_bytes.restype = ctypes.c_size_t
         L.aoh_extend.argtypes = [P(AohTensor)] * 3 + [ctypes.c_void_p] * 2 + caches + \
             [ctypes.c_int32, ctypes.c_int32, P(AohTensor), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
@@ -821,11 +821,12 @@ def aoh_kv_append_rope_varlen(q, k_new, v_new, cu_seqlens, max_new, rope, head_i
 
 # ----------------------------------------------------------------------------- running prompts
 
-def aoh_extend_workspace_bytes(batch, max_new, n_q_heads, n_kv_heads, d_head):
-    return int(lib().aoh_extend_workspace_bytes(batch, max_new, n_q_heads, n_kv_heads, d_head))
+def aoh_extend_workspace_bytes(batch, n_tokens, n_q_heads, n_kv_heads, d_head):
+    """Workspace of calls with n_tokens new tokens in all, in `batch` sequences."""
+    return int(lib().aoh_extend_workspace_bytes(batch, n_tokens, n_q_heads, n_kv_heads, d_head))
 
 
-def _extend(call, q, k_new, v_new, lead, seqs, longest, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, evict,
+def _extend(call, q, k_new, v_new, lead, seqs, tokens, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window, evict,
             append, out, workspace, stream):
     dev, d = _on_gpu(q, "q"), q.shape[-1]
     qd, kd, vd = _desc(q, "q", dev, d), _desc(k_new, "k_new", dev, d), _desc(v_new, "v_new", dev, d)
@@ -833,7 +834,7 @@ def _extend(call, q, k_new, v_new, lead, seqs, longest, head_is_streaming, start
     m = _q8_labels(head_is_streaming, k_new.shape[-2] if k_new.dim() > 1 else 0)
     full, ring = _cache_descs(kv_full, kv_ring, dev, d, q.dtype)
     if workspace is None:
-        n = aoh_extend_workspace_bytes(seqs, longest, q.shape[-2], k_new.shape[-2], d) if q.dim() > 1 and k_new.dim() > 1 else 0
+        n = aoh_extend_workspace_bytes(seqs, tokens, q.shape[-2], k_new.shape[-2], d) if q.dim() > 1 and k_new.dim() > 1 else 0
         workspace = _scratch(stream, torch.empty, n, dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"the workspace must be contiguous and on {dev}")
@@ -851,7 +852,7 @@ def aoh_extend(q, k_new, v_new, head_is_streaming, start_pos, kv_full, kv_ring, 
     caches.  evict: streaming heads see the cache as it was before the tokens (chunk eviction), else their per-token
     window."""
     b, n = (q.shape[0], q.shape[1]) if q.dim() > 1 else (1, 1)
-    return _extend("aoh_extend", q, k_new, v_new, (), b, n, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window,
+    return _extend("aoh_extend", q, k_new, v_new, (), b, b * n, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window,
                    evict, append, out, workspace, stream)
 
 
@@ -861,7 +862,7 @@ def aoh_extend_varlen(q, k_new, v_new, cu_seqlens, max_new, head_is_streaming, s
     max_new; rows behind the last sequence stay as they were."""
     n = cu_seqlens.numel() - 1
     cu = _q8_seqs(cu_seqlens, "cu_seqlens", q.device, 2) if n > 0 else None
-    return _extend("aoh_extend_varlen", q, k_new, v_new, (cu, n, max_new), n, max_new, head_is_streaming, start_pos, kv_full,
+    return _extend("aoh_extend_varlen", q, k_new, v_new, (cu, n, max_new), n, q.shape[0], head_is_streaming, start_pos, kv_full,
                    kv_ring, n_sink, window, evict, append, out, workspace, stream)
 
 

@@ -55,7 +55,7 @@ aoh_status extend_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
 
   const int cus = std::min(compute_units(), kWsMaxWgs / 2);
   if (dt == AOH_BF16) {
-    const size_t need = extend_workspace((int)D, kWsMaxWgs / 2);
+    const size_t need = extend_workspace(B, packed ? std::min(tokens, B * T) : tokens, (int)Hq, (int)Hkv, (int)D, kWsMaxWgs / 2);
     if (!workspace) return fail(AOH_ERR_WORKSPACE, "workspace is null; %zu bytes needed", need);
     if (workspace_bytes < need) return fail(AOH_ERR_WORKSPACE, "workspace has %zu bytes; %zu needed", workspace_bytes, need);
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(AOH_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
@@ -92,6 +92,7 @@ aoh_status extend_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
   std::memcpy(a.rank, hs.rank, sizeof(a.rank));
   std::memcpy(a.kv_heads, hs.ret, hs.n_ret);
   std::memcpy(a.kv_heads + hs.n_ret, hs.str, hs.n_str);
+  a.gs_mul = ((1ull << 36) + a.gs - 1) / a.gs;
   a.workspace = workspace;
   a.cus = cus;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -124,11 +125,11 @@ aoh_status extend_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
 
 extern "C" {
 
-size_t aoh_extend_workspace_bytes(int32_t batch, int32_t max_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head) {
-  if (batch < 1 || max_new < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads ||
+size_t aoh_extend_workspace_bytes(int32_t batch, int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head) {
+  if (batch < 1 || n_tokens < 1 || n_tokens > (1ll << 31) - 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads ||
       n_q_heads / n_kv_heads > 16 || (d_head != 64 && d_head != 128))
     return 0;
-  return extend_workspace(d_head, kWsMaxWgs / 2);
+  return extend_workspace(batch, n_tokens, n_q_heads, n_kv_heads, d_head, kWsMaxWgs / 2);
 }
 
 aoh_status aoh_extend(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,

@@ -260,6 +260,8 @@ struct RopeArgs {
 hipError_t launch_rope(const RopeArgs& a, int dtype, int d, bool append, hipStream_t s);
 
 // Attention of new tokens over the caches and themselves (extend.hip).
+struct ExtendHead;
+struct ExtendItem;
 struct ExtendArgs {
   const void* q;                // [B][T][H][D], or packed [total][H][D] (cu_seqlens; *_sb = 0)
   const void* k;
@@ -289,13 +291,19 @@ struct ExtendArgs {
   uint8_t kv_heads[kMaxKvHeads];  // retrieval heads, then streaming ones
   void* workspace;              // extend_workspace bytes (bf16)
   int32_t cus;                  // compute units
-  // set by the launcher: workgroups, the fewest tiles of one, and the partials of two blocks
-  // of rows a workgroup, [2 wgs][rows][D] and (m in log2 units, l)
+  uint64_t gs_mul;              // ceil(2^36 / gs)
+  // set by the launcher: workgroups, the fewest tiles of one; the partials of two blocks of
+  // rows a workgroup, [2 wgs][rows][D] and (m in log2 units, l); the plan
   int32_t wgs, min_tiles;
   float* part_acc;
   float* part_ml;
+  ExtendHead* head;
+  ExtendItem* items;
+  int32_t* first_item;          // by range, the item that it starts in
+  ExtendArgs* copy;             // these arguments, in device memory
 };
-size_t extend_workspace(int d, int cus);
+// Workspace of calls with so many new tokens in so many sequences.
+size_t extend_workspace(int64_t batch, int64_t tokens, int hq, int hkv, int d, int cus);
 hipError_t launch_extend(const ExtendArgs& a, int dtype, int d, hipStream_t s);
 
 // The head classifier over L layers.  Weights are bf16 [L][H * D][d_model]

@@ -51,67 +51,241 @@ __device__ __forceinline__ int ring_position(int c, int start, int n_sink, int w
 // The work space.  An item's places: kUnit for each tile that its rows visit, about (a
 // first number and a step from one block of rows to the next), and kItemCost tiles for its
 // start.  A range of places stands for the same share of the item's visits, so the numbers
-// need not be exact.
+// need not be exact.  A first launch writes the items and where every range starts, so that
+// the others begin with a few scalar loads.
 constexpr int kUnit = 16;
-constexpr int kItemCost = 1;
-constexpr int kPlanSeqs = 64;  // sequences of a launch, one a lane; larger batches go in parts
+constexpr int kItemCost = 3;
+constexpr int kPlanSeqs = 1024;  // sequences of a launch; larger batches go in parts
 
-struct ExtendPlan {
-  int64_t n_ret_places, total;  // places of the retrieval items, of all items
-  int64_t range;                // places of a workgroup
-  int used;                     // workgroups with a range
-  // this lane's sequence: first places of its retrieval and streaming items, places of one
-  // head's items, of the first block of rows, and the step
-  int64_t ret0, ret_head, ret_a, str0, str_head, str_a;
-  int ret_c, str_c;
-  int blocks;  // blocks of rows
+struct ExtendHead {
+  int64_t total, range;  // places of all items, of a range
+  int32_t used, n_items; // ranges, items
 };
 
-__device__ __forceinline__ int64_t lane_scan(int64_t x) {
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
+struct ExtendItem {
+  int64_t first, places;
+  // element offsets of the sequence's first new token (query head: the group's first), of its
+  // row of the block table, and of its ring
+  int64_t q_off, k_off, v_off, o_off, table, ring;
+  // Visits: tile = visit + (0 below c1, o1 below c2, o2) among the n_cached of the cache, then
+  // counted from there + (0 below d1, e1) among the new ones; n in all.
+  int32_t n, n_cached, c1, c2, o1, o2, d1, e1;
+  int32_t start, cached, n_new, row0;   // tokens before, positions (slots) that the cache holds, new tokens, first row
+  int32_t t_first, t_last;              // tokens of its rows
+  // First key of token t's window: lo_off + t (far below where there is none).  Ring: offset r
+  // behind the sinks holds position rbase + r, one window less behind r = rrem.
+  int32_t lo_off, rbase, rrem;
+  int32_t str, head, rank;              // streaming; KV head, and its rank in its cache
+
+  __device__ __forceinline__ int tile(int it) const {
+    if (it < n_cached) return it + (it < c1 ? 0 : it < c2 ? o1 : o2);
+    const int j = it - n_cached;
+    return j + (j < d1 ? 0 : e1);
   }
-  return x;
+};
+
+// A value that all lanes share, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  const uint32_t lo = (uint32_t)uniform((int)(uint32_t)x), hi = (uint32_t)uniform((int)(uint32_t)(x >> 32));
+  return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
+// A load from a uniform address into scalar registers: it is waited for with the LDS reads,
+// not with the direct loads.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+  static_assert(sizeof(T) % 4 == 0, "whole words");
+  typedef const __attribute__((address_space(4))) uint32_t* words;
+  const words w = (words)uniform((uint64_t)reinterpret_cast<uintptr_t>(p));
+  uint32_t x[sizeof(T) / 4];
+#pragma unroll
+  for (size_t i = 0; i < sizeof(T) / 4; ++i) x[i] = w[i];
+  return __builtin_bit_cast(T, x);
 }
+
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
+// x / y of numbers below 2^53 (a 64-bit division is many times longer).
+__device__ __forceinline__ int64_t div64(int64_t x, int64_t y) {
+  int64_t q = (int64_t)((double)x / (double)y);
+  const int64_t r = x - q * y;
+  if (r < 0) --q;
+  else if (r >= y) ++q;
+  return q;
+}
+// x / gs for the rows of an item (x < 2^30): exact, as gs <= 16.
+__device__ __forceinline__ int div_gs(const ExtendArgs& a, int x) { return (int)(((uint64_t)(uint32_t)x * a.gs_mul) >> 36); }
+
 // Places of the first n of an item's blocks of rows.
 __device__ __forceinline__ int64_t places_of(int64_t a, int c, int64_t n) { return n * a + c * (n * (n - 1) / 2); }
 
+// Blocks of rows of a sequence, places of a block of rows of its retrieval and its streaming
+// heads: first block, step.
+struct SeqCost {
+  int blocks;
+  int64_t a[2];
+  int c[2];
+};
+
 template <int ROWS, int TILE>
-__device__ __forceinline__ ExtendPlan extend_plan(const ExtendArgs& a) {
-  const int lane = threadIdx.x & (kWave - 1);
-  ExtendPlan p;
-  ExtendSeq s = {0, 0, 0};
-  if (lane < a.B) s = extend_seq(a, lane);
-  p.blocks = (int)(((int64_t)s.n * a.gs + ROWS - 1) / ROWS);
+__device__ __forceinline__ SeqCost seq_cost(const ExtendArgs& a, const ExtendSeq& s) {
+  SeqCost x;
+  x.blocks = (int)(((int64_t)s.n * a.gs + ROWS - 1) / ROWS);
   const int step = max(1, kUnit * ROWS / (TILE * a.gs));  // new tiles that the next block of rows sees more
   const int n_new = div_up(s.n, TILE), first = div_up(div_up(ROWS, a.gs), TILE);
   const int paged = div_up(min(s.start, a.max_pages * kPage), TILE);
   const int ring = div_up(min(s.start, a.ring_cap), TILE);
-  p.ret_a = (int64_t)kUnit * (kItemCost + paged + min(n_new, first));
-  p.ret_c = step;
+  x.a[0] = (int64_t)kUnit * (kItemCost + paged + min(n_new, first));
+  x.c[0] = step;
   // the band of a block has at most window + tokens of the block keys
   const int band = div_up(a.n_sink, TILE) + div_up(a.window, TILE) + first + 1;
-  p.str_a = (int64_t)kUnit * (kItemCost + (a.evict ? ring + min(n_new, first) : min(ring + n_new, band)));
-  p.str_c = a.evict ? step : 0;
-  p.ret_head = places_of(p.ret_a, p.ret_c, p.blocks);
-  p.str_head = places_of(p.str_a, p.str_c, p.blocks);
-  const int64_t ret = a.n_ret * p.ret_head, str = a.n_str * p.str_head;
-  const int64_t ret_to = lane_scan(ret), str_to = lane_scan(str);
-  p.n_ret_places = from_lane(ret_to, kWave - 1);
-  p.total = p.n_ret_places + from_lane(str_to, kWave - 1);
-  p.ret0 = ret_to - ret;
-  p.str0 = p.n_ret_places + str_to - str;
-  p.range = max((p.total + a.wgs - 1) / a.wgs, (int64_t)a.min_tiles * kUnit);
-  p.used = (int)((p.total + p.range - 1) / p.range);
-  return p;
+  x.a[1] = (int64_t)kUnit * (kItemCost + (a.evict ? ring + min(n_new, first) : min(ring + n_new, band)));
+  x.c[1] = a.evict ? step : 0;
+  return x;
+}
+
+// Fills in the tiles that rows of tokens t_first .. t_last visit.
+template <int TILE>
+__device__ __forceinline__ void set_visits(const ExtendArgs& a, ExtendItem& x) {
+  const int all = div_up(x.cached, TILE), n_new = x.t_last / TILE + 1;
+  x.o1 = x.o2 = x.d1 = x.e1 = 0;
+  x.lo_off = INT32_MIN / 2;
+  x.rbase = x.rrem = 0;
+  if (!x.str) {
+    x.n_cached = x.c1 = x.c2 = all;
+    x.n = all + n_new;
+    return;
+  }
+  const int start = x.start;
+  if (!a.evict) x.lo_off = start - a.window + 1;
+  const int rlast = max(start - 1 - a.n_sink, 0);
+  x.rrem = rlast % a.window;
+  x.rbase = a.n_sink + rlast - x.rrem;
+  const int lo = a.evict ? start - a.window : start + x.t_first - a.window + 1;
+  const int w0 = max(lo, a.n_sink);  // first cached position of the window
+  const int sinks = div_up(min(a.n_sink, x.cached), TILE);
+  int f1 = sinks, l1 = sinks, f2 = 0, l2 = 0;  // runs of window tiles
+  if (w0 < start) {
+    const int p = a.n_sink + (w0 - a.n_sink) % a.window, q = a.n_sink + (start - 1 - a.n_sink) % a.window;
+    if (start - w0 >= a.window) {
+      l1 = all;
+    } else if (p <= q) {
+      f1 = max(sinks, p / TILE);
+      l1 = q / TILE + 1;
+    } else {
+      f1 = max(sinks, a.n_sink / TILE);
+      l1 = q / TILE + 1;
+      f2 = max(max(f1, l1), p / TILE);
+      l2 = all;
+    }
+  }
+  x.c1 = sinks;
+  x.c2 = sinks + max(0, l1 - f1);
+  x.n_cached = x.c2 + max(0, l2 - f2);
+  x.o1 = f1 - x.c1;
+  x.o2 = f2 - x.c2;
+  const int d0 = max(0, lo - start) / TILE;  // first new tile of the window
+  x.d1 = min(div_up(max(0, a.n_sink - start), TILE), d0);
+  x.e1 = d0 - x.d1;
+  x.n = x.n_cached + x.d1 + n_new - d0;
+}
+
+// Items go by head type, sequence, KV head and block of rows.  Every workgroup scans the
+// sequences (four a thread), each thread then writes items.
+template <int ROWS, int TILE>
+__global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
+  __shared__ int64_t s_places[2][kPlanSeqs + 1];
+  __shared__ int s_blocks[kPlanSeqs + 1];
+  __shared__ int64_t s_wave[3][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_kv[2] = {a.n_ret, a.n_str};
+  int64_t x[3][4], sum[3] = {0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int b = 4 * tid + u;
+    ExtendSeq s = {0, 0, 0};
+    if (b < a.B) s = extend_seq(a, b);
+    const SeqCost k = seq_cost<ROWS, TILE>(a, s);
+    x[0][u] = n_kv[0] * places_of(k.a[0], k.c[0], k.blocks);
+    x[1][u] = n_kv[1] * places_of(k.a[1], k.c[1], k.blocks);
+    x[2][u] = k.blocks;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sum[i] += x[i][u];
+  }
+  int64_t inc[3] = {sum[0], sum[1], sum[2]};
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int64_t y = __shfl_up(inc[i], o, kWave);
+      if (lane >= o) inc[i] += y;
+    }
+  if (lane == kWave - 1)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) s_wave[i][wave] = inc[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    int64_t at = inc[i] - sum[i];
+    for (int w = 0; w < wave; ++w) at += s_wave[i][w];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i < 2) s_places[i][4 * tid + u] = at;
+      else s_blocks[4 * tid + u] = (int)at;
+      at += x[i][u];
+    }
+    if (tid == 255) {
+      if (i < 2) s_places[i][kPlanSeqs] = at;
+      else s_blocks[kPlanSeqs] = (int)at;
+    }
+  }
+  __syncthreads();
+  const int blocks = s_blocks[kPlanSeqs];
+  const int n_items = (n_kv[0] + n_kv[1]) * blocks;
+  const int64_t total = s_places[0][kPlanSeqs] + s_places[1][kPlanSeqs];
+  const int64_t range = max(div64(total + a.wgs - 1, a.wgs), (int64_t)a.min_tiles * kUnit);
+  const int used = (int)div64(total + range - 1, range);
+  if (blockIdx.x == 0 && tid == 0) {
+    *a.head = ExtendHead{total, range, used, n_items};
+    *a.copy = a;
+  }
+  for (int idx = blockIdx.x * 256 + tid; idx < n_items; idx += gridDim.x * 256) {
+    ExtendItem it;
+    it.str = idx >= n_kv[0] * blocks;
+    const int heads = n_kv[it.str], at = idx - (it.str ? n_kv[0] * blocks : 0);
+    int b = 0;  // the last sequence whose items begin at or before this one (and has some)
+    for (int hi = kPlanSeqs; hi - b > 1;) {
+      const int mid = (b + hi) >> 1;
+      if ((int64_t)heads * s_blocks[mid] <= at) b = mid;
+      else hi = mid;
+    }
+    const ExtendSeq s = extend_seq(a, b);
+    const SeqCost k = seq_cost<ROWS, TILE>(a, s);
+    const int64_t ka = k.a[it.str];
+    const int kc = k.c[it.str];
+    const int in_seq = at - heads * s_blocks[b];
+    it.rank = in_seq / k.blocks;
+    const int rb = in_seq - it.rank * k.blocks;
+    it.first = (it.str ? s_places[0][kPlanSeqs] : 0) + s_places[it.str][b] + it.rank * places_of(ka, kc, k.blocks) + places_of(ka, kc, rb);
+    it.places = ka + (int64_t)kc * rb;
+    it.head = a.kv_heads[it.str ? a.n_ret + it.rank : it.rank];
+    const int64_t sb = a.cu_seqlens ? 0 : b, tok0 = a.cu_seqlens ? s.row0 : 0;
+    it.q_off = sb * a.q_sb + tok0 * a.q_st + (int64_t)it.head * a.gs * a.q_sh;
+    it.k_off = sb * a.k_sb + tok0 * a.k_st + it.head * a.k_sh;
+    it.v_off = sb * a.v_sb + tok0 * a.v_st + it.head * a.v_sh;
+    it.o_off = sb * a.o_sb + tok0 * a.o_st + (int64_t)it.head * a.gs * a.o_sh;
+    it.table = (int64_t)b * a.max_pages;
+    it.ring = ((int64_t)b * a.n_str + it.rank) * a.ring_blocks;
+    it.start = s.start;
+    it.n_new = s.n;
+    it.cached = it.str ? min(s.start, a.ring_cap) : min(s.start, a.max_pages * kPage);
+    it.row0 = rb * ROWS;
+    it.t_first = div_gs(a, it.row0);
+    it.t_last = div_gs(a, min(it.row0 + ROWS, s.n * a.gs) - 1);
+    set_visits<TILE>(a, it);
+    a.items[idx] = it;
+    // ranges that start in this item
+    for (int w = (int)div64(it.first + range - 1, range); w < used && w * range < it.first + it.places; ++w) a.first_item[w] = idx;
+  }
 }
 
 // Ranges go to the 8 XCDs (each with its own L2) in eight consecutive parts, so that the
@@ -119,96 +293,6 @@ __device__ __forceinline__ ExtendPlan extend_plan(const ExtendArgs& a) {
 __device__ __forceinline__ int range_of(int w, int used) {
   const int per = (used + 7) >> 3, r = (w & 7) * per + (w >> 3);
   return (w >> 3) < per && r < used ? r : -1;
-}
-
-struct ExtendItem {
-  int b, kvl, rb;  // sequence, rank of the KV head in its cache, block of rows
-  bool str;
-  int64_t first, places;
-};
-
-// The item that holds place g < total.
-__device__ __forceinline__ ExtendItem extend_item(const ExtendPlan& p, int64_t g, int n_ret, int n_str) {
-  ExtendItem it;
-  it.str = g >= p.n_ret_places;
-  const int64_t at = it.str ? p.str0 : p.ret0, head = it.str ? p.str_head : p.ret_head;
-  const uint64_t hit = __ballot(g >= at && g < at + head * (it.str ? n_str : n_ret));
-  it.b = hit ? __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit)) : 0;
-  const int64_t at_b = from_lane(at, it.b), head_b = from_lane(head, it.b);
-  const int64_t a = from_lane(it.str ? p.str_a : p.ret_a, it.b);
-  const int c = __builtin_amdgcn_readlane(it.str ? p.str_c : p.ret_c, it.b);
-  it.kvl = (int)((g - at_b) / head_b);
-  const int64_t base = at_b + it.kvl * head_b, off = g - base;
-  int lo = 0, hi = __builtin_amdgcn_readlane(p.blocks, it.b);  // the last block that starts at or before off
-  if (c == 0) {
-    lo = (int)(off / a);
-  } else {
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (places_of(a, c, mid) <= off) lo = mid;
-      else hi = mid;
-    }
-  }
-  it.rb = lo;
-  it.first = base + places_of(a, c, lo);
-  it.places = a + (int64_t)c * lo;
-  return it;
-}
-
-// The tiles that an item's rows visit: up to three runs of cached tiles, then up to two of
-// new ones.
-struct Visits {
-  int n_cached, n;          // visits of the cache, all visits
-  int c1, c2, o0, o1, o2;   // cached: tile = visit + o0 below c1, + o1 below c2, + o2
-  int d1, e0, e1;           // new: the same with the visit's place behind n_cached
-  __device__ __forceinline__ int tile(int it) const {
-    if (it < n_cached) return it + (it < c1 ? o0 : it < c2 ? o1 : o2);
-    const int j = it - n_cached;
-    return j + (j < d1 ? e0 : e1);
-  }
-};
-
-// Rows of tokens t0 .. t1 of a sequence; cached: what its cache holds (positions, or slots).
-template <int TILE>
-__device__ __forceinline__ Visits visits_of(const ExtendArgs& a, bool str, int start, int cached, int t0, int t1) {
-  Visits v;
-  const int all = div_up(cached, TILE), n_new = t1 / TILE + 1;
-  v.o0 = v.o1 = v.o2 = v.e0 = v.e1 = 0;
-  if (!str) {
-    v.n_cached = v.c1 = v.c2 = all;
-    v.d1 = n_new;
-    v.n = all + n_new;
-    return v;
-  }
-  const int lo = a.evict ? start - a.window : start + t0 - a.window + 1;
-  const int w0 = max(lo, a.n_sink);  // first cached position of the window
-  const int sinks = div_up(min(a.n_sink, cached), TILE);
-  int f1 = sinks, l1 = sinks, f2 = 0, l2 = 0;  // runs of window tiles
-  if (w0 < start) {
-    const int x = a.n_sink + (w0 - a.n_sink) % a.window, y = a.n_sink + (start - 1 - a.n_sink) % a.window;
-    if (start - w0 >= a.window) {
-      l1 = all;
-    } else if (x <= y) {
-      f1 = max(sinks, x / TILE);
-      l1 = y / TILE + 1;
-    } else {
-      f1 = max(sinks, a.n_sink / TILE);
-      l1 = y / TILE + 1;
-      f2 = max(max(f1, l1), x / TILE);
-      l2 = all;
-    }
-  }
-  v.c1 = sinks;
-  v.c2 = sinks + max(0, l1 - f1);
-  v.n_cached = v.c2 + max(0, l2 - f2);
-  v.o1 = f1 - v.c1;
-  v.o2 = f2 - v.c2;
-  const int d0 = max(0, lo - start) / TILE;  // first new tile of the window
-  const int new_sinks = min(div_up(max(0, a.n_sink - start), TILE), d0);
-  v.d1 = new_sinks;
-  v.e1 = d0 - new_sinks;
-  v.n = v.n_cached + new_sinks + n_new - d0;
-  return v;
 }
 
 // Four output values at element `at`.
@@ -392,10 +476,18 @@ struct TileRing {
 // reference max, that is accepted as it is.
 constexpr float kSumHi = 65536.f;
 
-// A block table entry, by a scalar load (the address is uniform): it is waited for with the
-// LDS reads, not with the direct loads.
-__device__ __forceinline__ int scalar_i32(const int32_t* p) {
-  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+// Direct loads, 16 bytes a lane to lds_row + 16 lane (see lds_dma16): from a uniform address
+// plus a lane's byte offset, and from a lane's address.  The hazards that the compiler does
+// not see inside the assembly are waited for there: an address in scalar registers that a
+// vector instruction has just written (five cycles), M0 just written (one).
+__device__ __forceinline__ void lds_dma16_from(const void* base, uint32_t offset, const void* lds_row) {
+  const uint32_t m0 = (uint32_t)uniform((int)reinterpret_cast<uintptr_t>(lds_row));
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(uniform((uint64_t)reinterpret_cast<uintptr_t>(base))), "{m0}"(m0) : "memory");
+}
+
+__device__ __forceinline__ void lds_dma16_at(const void* gptr, const void* lds_row) {
+  const uint32_t m0 = (uint32_t)uniform((int)reinterpret_cast<uintptr_t>(lds_row));
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr), "{m0}"(m0) : "memory");
 }
 
 __device__ __forceinline__ bool not_finite(u32x4 x) {
@@ -437,6 +529,19 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
   const uint32_t kaddr0 = kring0 + 2u * (uint32_t)Tile::koff(krow0, h2);
   const uint32_t vaddr0 = vring0 + 2u * (uint32_t)(Tile::voff(8 * h2 + (i16 >> 2), 2 * (q16 & 1) + ((i16 & 3) >> 1)) + 4 * (i16 & 1));
   const uint32_t paddr0 = vring0 + 32u * l32 + 16u * (h2 ^ ((l32 >> 3) & 1));
+  // Direct loads of a tile: wave w fills kLoads blocks of 1 KB of K and of V, one instruction
+  // each, which lie in one page of the tile (my_page): byte offsets in the page, and rows of
+  // the tile.
+  constexpr int kBlockRows = 512 / D;
+  const int my_page = wave * Shape::kLoads * kBlockRows / kPage;
+  uint32_t dma_k[Shape::kLoads];
+#pragma unroll
+  for (int jj = 0; jj < Shape::kLoads; ++jj) {
+    const int r = kBlockRows * (Shape::kLoads * wave + jj) + lane / Tile::kChunks;
+    dma_k[jj] = 2u * ((r % kPage) * D + 8 * ((lane % Tile::kChunks) ^ Tile::kx(r)));
+  }
+  const int dim0 = (32 * Shape::kLoads * wave + (lane >> 1)) % D, half0 = (lane & 1) ^ ((dim0 >> 3) & 1);
+  const uint32_t dma_v = 2u * (dim0 * kPage + 8 * half0);
   auto k_operand = [&](uint32_t at, int s, int blk) __attribute__((always_inline)) {
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
     return *reinterpret_cast<lds_bf16x8*>((at ^ (32u * s)) + 64u * D * blk);
@@ -460,30 +565,18 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  const ExtendHead head = scalar_load(a.head);
+  const int rng = range_of(blockIdx.x, head.used);
+  if (rng < 0) return false;
+  const int64_t g1 = min((rng + 1) * head.range, head.total);
+  int64_t g0 = rng * head.range;
   bool again = false;
-  int64_t g0 = -1;
 #pragma unroll 1
-  for (;;) {
-    // The plan is made anew for every item, which costs less than the registers that would
-    // hold it through the tiles.
-    const ExtendPlan plan = extend_plan<ROWS, kBN>(a);
-    const int rng = range_of(blockIdx.x, plan.used);
-    if (rng < 0) return false;
-    const int64_t g1 = min((rng + 1) * plan.range, plan.total);
-    if (g0 < 0) g0 = rng * plan.range;
-    if (g0 >= g1) return again;
-    const ExtendItem item = extend_item(plan, g0, a.n_ret, a.n_str);
-    const ExtendSeq seq = extend_seq(a, item.b);
-    const bool str = item.str;
-    const int g = a.kv_heads[str ? a.n_ret + item.kvl : item.kvl];
-    const int start = __builtin_amdgcn_readfirstlane(seq.start), n_new = __builtin_amdgcn_readfirstlane(seq.n);
-    const int n_rows = n_new * a.gs, row0 = item.rb * ROWS;
-    const int cached = str ? min(start, a.ring_cap) : min(start, a.max_pages * kPage);
-    const int t_first = row0 / a.gs, t_last = (min(row0 + ROWS, n_rows) - 1) / a.gs;
-    const Visits vis = visits_of<kBN>(a, str, start, cached, t_first, t_last);
-    // the share of the visits that this range stands for
+  for (int idx = scalar_load(a.first_item + rng); g0 < g1; ++idx) {
+    const ExtendItem item = scalar_load(a.items + idx);
+    // the share of the item's visits that this range stands for
     const int64_t s0 = g0 - item.first, s1 = min(g1 - item.first, item.places);
-    const int v0 = (int)(s0 * vis.n / item.places), v1 = (int)(s1 * vis.n / item.places);
+    const int v0 = uniform((int)div64(s0 * item.n, item.places)), v1 = uniform((int)div64(s1 * item.n, item.places));
     const bool whole = s0 == 0 && s1 == item.places;
     g0 = item.first + s1;
     const int64_t part = (int64_t)(2 * rng + (s0 == 0 ? 1 : 0)) * ROWS;
@@ -494,74 +587,68 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       }
       continue;
     }
-
+    const int start = item.start, n_new = item.n_new, cached = item.cached, lo_off = item.lo_off;
+    const bool str = item.str, band = str && !a.evict;
+    const int n_rows = n_new * a.gs;
     // This lane's row, and the wave's first and last tokens.
-    const int my_r = min(row0 + wave * 32 + l32, n_rows - 1);
-    const int my_t = my_r / a.gs;
-    const int w_t0 = min(row0 + wave * 32, n_rows - 1) / a.gs, w_t1 = min(row0 + wave * 32 + 31, n_rows - 1) / a.gs;
-    // Without a window of its own (retrieval, or a window that no key has left) nothing is
-    // below a row's first key.
-    const bool band = str && !a.evict;
-    const int lo_off = band ? start - a.window + 1 : INT32_MIN / 2;  // first key of token t's window: lo_off + t
-    // ring: offset r behind the sinks holds position rbase + r, one window less behind r = rrem
-    const int rlast = max(start - 1 - a.n_sink, 0), rrem = rlast % a.window, rbase = a.n_sink + rlast - rrem;
-    const int64_t sb = a.cu_seqlens ? 0 : item.b, tok0 = a.cu_seqlens ? seq.row0 : 0;
-    const uint16_t* kn = static_cast<const uint16_t*>(a.k) + sb * a.k_sb + tok0 * a.k_st + g * a.k_sh;
-    const uint16_t* vn = static_cast<const uint16_t*>(a.v) + sb * a.v_sb + tok0 * a.v_st + g * a.v_sh;
-    // cached tiles: units of 16 rows, `unit_step` apart from one page (block) to the next
-    const int unit_step = str ? 1 : a.n_ret;
-    const int64_t unit0 = str ? ((int64_t)item.b * a.n_str + item.kvl) * a.ring_blocks : item.kvl;
+    const int my_r = min(item.row0 + wave * 32 + l32, n_rows - 1);
+    const int my_t = div_gs(a, my_r);
+    const int w_t0 = div_gs(a, min(item.row0 + wave * 32, n_rows - 1)), w_t1 = div_gs(a, min(item.row0 + wave * 32 + 31, n_rows - 1));
+    const int64_t q_at = item.q_off + my_t * a.q_st + (my_r - my_t * a.gs) * a.q_sh;
+    const uint16_t* kn = static_cast<const uint16_t*>(a.k) + item.k_off;
+    const uint16_t* vn = static_cast<const uint16_t*>(a.v) + item.v_off;
+    // cached tiles: units of 16 rows, unit_step elements from one page (block) to the next
+    const int unit_step = (str ? 1 : a.n_ret) * (kPage * D);
+    const int64_t unit0 = str ? item.ring : item.rank;
     const uint16_t* kc = static_cast<const uint16_t*>(str ? a.rk : a.pk) + unit0 * (kPage * D);
     const uint16_t* vc = static_cast<const uint16_t*>(str ? a.rv : a.pv) + unit0 * (kPage * D);
-    const int32_t* table = str ? nullptr : a.block_table + (int64_t)item.b * a.max_pages;
+    const int32_t* table = a.block_table + item.table;
     const int last_page = max(div_up(cached, kPage) - 1, 0);
     const int end_page = str ? a.ring_blocks : a.num_pages;
-
-    // Direct loads of a tile: wave w fills kLoads blocks of 1 KB of K and of V, one
-    // instruction each, which lie in one page of the tile (my_page).
-    constexpr int kBlockRows = 512 / D;
-    const int my_page = wave * Shape::kLoads * kBlockRows / kPage;
+    int64_t k_st = a.k_st, v_st = a.v_st;
+    int n_sink = a.n_sink, window = a.window;
+    // registers of their own, not those of the argument block's load
+    if constexpr (!CAREFUL) asm("" : "+s"(k_st), "+s"(v_st), "+s"(n_sink), "+s"(window));
     bool bad = false;  // this wave has met a page outside the cache, or a V that the fast loop cannot take
     // Page of this wave's part of a cached tile: the block table's entry, read ahead of its use.
     auto entry_of = [&](int it) __attribute__((always_inline)) {
-      const int pg = min(vis.tile(it) * (kBN / kPage) + my_page, last_page);
-      return table ? scalar_i32(table + pg) : pg;
+      const int pg = min(item.tile(it) * (kBN / kPage) + my_page, last_page);
+      return str ? pg : scalar_load(table + pg);
     };
-    auto issue_cached = [&](int slot_k, int slot_v, int entry) __attribute__((always_inline)) {
+    auto issue_cached = [&](int slot_k, int slot_v, int entry_v) __attribute__((always_inline)) {
+      int entry = uniform(entry_v);
       if (entry < 0 || entry >= end_page) {
         bad = true;
         entry = 0;
       }
-      const int64_t unit = (int64_t)entry * unit_step * (kPage * D);
+      const int64_t unit = (int64_t)entry * unit_step;
       const uint16_t* ku = kc + unit;
       const uint16_t* vu = vc + unit;
 #pragma unroll
       for (int jj = 0; jj < Shape::kLoads; ++jj) {
         const int j = Shape::kLoads * wave + jj;
-        const int r = kBlockRows * j + lane / Tile::kChunks;  // row of the tile
-        lds_dma16(ku + (r % kPage) * D + 8 * ((lane % Tile::kChunks) ^ Tile::kx(r)), &ring.k[slot_k][512 * j]);
-        const int dim = (32 * j + (lane >> 1)) % D;
-        lds_dma16(vu + dim * kPage + 8 * ((lane & 1) ^ ((dim >> 3) & 1)), &ring.v[slot_v][512 * j]);
+        lds_dma16_from(ku, dma_k[jj], &ring.k[slot_k][512 * j]);
+        lds_dma16_from(vu, dma_v + 1024 * jj, &ring.v[slot_v][512 * j]);
       }
     };
     auto issue_new = [&](int it, int slot_k, int slot_v) __attribute__((always_inline)) {
-      const int kb = vis.tile(it) * kBN;
+      const int kb = item.tile(it) * kBN;
 #pragma unroll
       for (int jj = 0; jj < Shape::kLoads; ++jj) {
         const int j = Shape::kLoads * wave + jj;
         const int r = kBlockRows * j + lane / Tile::kChunks, pc = lane % Tile::kChunks;
         const int64_t row = min(kb + r, n_new - 1);  // rows behind the last repeat it; no query sees them
-        lds_dma16(kn + row * a.k_st + 8 * (pc ^ Tile::kx(r)), &ring.k[slot_k][512 * j]);
-        lds_dma16(vn + row * a.v_st + 8 * (pc ^ Tile::vx(r)), &ring.v[slot_v][512 * j]);
+        lds_dma16_at(kn + row * k_st + 8 * (pc ^ Tile::kx(r)), &ring.k[slot_k][512 * j]);
+        lds_dma16_at(vn + row * v_st + 8 * (pc ^ Tile::vx(r)), &ring.v[slot_v][512 * j]);
       }
     };
     // V of a tile that this wave's loads have brought: zeroes tokens behind the cache's last
     // one, and looks for values that are not finite where a row does not see all keys.
     auto clean = [&](int it, int slot_v) __attribute__((always_inline)) {
-      const int kb = vis.tile(it) * kBN;
-      const bool of_cache = it < vis.n_cached;
+      const int kb = item.tile(it) * kBN;
+      const bool of_cache = it < item.n_cached;
       const bool tail = of_cache && kb + kBN > cached;
-      const bool masked = of_cache ? band : kb + kBN - 1 > t_first || !(start + kb + kBN - 1 < a.n_sink || start + kb >= lo_off + t_last);
+      const bool masked = of_cache ? band : kb + kBN - 1 > item.t_first || !(start + kb + kBN - 1 < n_sink || start + kb >= lo_off + item.t_last);
       if (!tail && !masked) return;
 #pragma unroll
       for (int jj = 0; jj < Shape::kLoads; ++jj) {
@@ -569,8 +656,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         u32x4* at = reinterpret_cast<u32x4*>(&ring.v[slot_v][512 * j + 8 * lane]);
         u32x4 x = *at;
         if (tail) {
-          const int dim = (32 * j + (lane >> 1)) % D;
-          const int left = cached - (kb + (32 * j / D) * kPage + 8 * ((lane & 1) ^ ((dim >> 3) & 1)));
+          const int left = cached - (kb + (32 * j / D) * kPage + 8 * half0);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = left >= 2 * e + 2 ? x[e] : left == 2 * e + 1 ? x[e] & 0xffffu : 0u;
           *at = x;
@@ -646,10 +732,10 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     // Whether this lane's row sees key j (position, slot, or new token).
     auto sees = [&](bool of_cache, int j) __attribute__((always_inline)) {
       if (of_cache) {
-        const int r = j - a.n_sink;
-        return j < cached && (r < 0 || rbase + r - (r > rrem ? a.window : 0) >= lo_off + my_t);
+        const int r = j - n_sink;
+        return (j < cached) & ((r < 0) | (item.rbase + r - (r > item.rrem ? window : 0) >= lo_off + my_t));
       }
-      return j <= my_t && (start + j < a.n_sink || start + j >= lo_off + my_t);
+      return (j <= my_t) & ((start + j < n_sink) | (start + j >= lo_off + my_t));
     };
     auto apply_mask = [&](bool of_cache, int kb) __attribute__((always_inline)) {
 #pragma unroll
@@ -711,13 +797,13 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     if constexpr (!CAREFUL) {
       auto valu_phase = [&](auto is_cached, int it) __attribute__((always_inline)) {
         constexpr bool of_cache = decltype(is_cached)::value;
-        const int kb = vis.tile(it) * kBN;
+        const int kb = item.tile(it) * kBN;
         bool dead = false, mask;
         if constexpr (of_cache) {
           mask = kb + kBN > cached || band;
         } else {
-          dead = kb > w_t1 || (start + kb >= a.n_sink && start + kb + kBN - 1 < lo_off + w_t0);
-          mask = kb + kBN - 1 > w_t0 || !(start + kb + kBN - 1 < a.n_sink || start + kb >= lo_off + w_t1);
+          dead = kb > w_t1 || (start + kb >= n_sink && start + kb + kBN - 1 < lo_off + w_t0);
+          mask = kb + kBN - 1 > w_t0 || !(start + kb + kBN - 1 < n_sink || start + kb >= lo_off + w_t1);
         }
         if (dead) {  // no row of the wave sees a key
 #pragma unroll
@@ -738,13 +824,13 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       auto next_v = [&](int& x) __attribute__((always_inline)) { x = x + 1 == Shape::kVSlots ? 0 : x + 1; };
       int entry = 0;  // of the next tile that is loaded, if it is cached
       auto issue = [&](int it) __attribute__((always_inline)) {
-        if (it < vis.n_cached) issue_cached(in_k, in_v, entry);
+        if (it < item.n_cached) issue_cached(in_k, in_v, entry);
         else issue_new(it, in_k, in_v);
         next_k(in_k);
         next_v(in_v);
       };
       auto read_entry = [&](int it) __attribute__((always_inline)) {
-        if (it < vis.n_cached && it < v1) entry = entry_of(it);
+        if (it < item.n_cached && it < v1) entry = entry_of(it);
       };
       // The barrier of a tile follows each wave's wait for its loads of the next one (with
       // loads three tiles ahead those of the one after may stay in flight); after it, the
@@ -768,14 +854,13 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         issue(v0 + u);
       }
       {
-        const int my_h = g * a.gs + my_r % a.gs;
-        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + sb * a.q_sb + (tok0 + my_t) * a.q_st + my_h * a.q_sh;
+        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + q_at;
 #pragma unroll
         for (int s = 0; s < kKSteps; ++s) qreg[s] = __builtin_bit_cast(bf16x8, ld16(qp + 8 * h2 + 16 * s));
       }
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
       clean(v0, 0);
-      read_entry(v0 + Shape::kAhead);
+      if (grp == 1) read_entry(v0 + Shape::kAhead);
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       barrier();
 
@@ -783,31 +868,27 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       // after its vector phase, waves 4-7 after its MFMA phase.  A block table entry is read
       // while the vector phase runs.
       auto vector_phase = [&](auto is_cached, int it) __attribute__((always_inline)) {
-        if (grp == 1) {
-          sync_tile(it);
-          read_entry(it + 1 + Shape::kAhead);
-        }
+        if (grp == 1) sync_tile(it);
+        read_entry(it + grp + Shape::kAhead);
         valu_phase(is_cached, it);
-        if (grp == 0) {
-          sync_tile(it);
-          read_entry(it + 1 + Shape::kAhead);
-        }
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+        if (grp == 0) sync_tile(it);
       };
       auto run_tiles = [&](auto is_cached, int i0, int i1) __attribute__((always_inline)) {
         qk_part(at_k);
         next_k(at_k);
-        vector_phase(is_cached, i0);
 #pragma unroll 1
-        for (int it = i0 + 1; it < i1; ++it) {
+        for (int it = i0;;) {
+          vector_phase(is_cached, it);
+          if (++it == i1) break;
           mfma_phase(is_cached, at_k, at_v);
           next_k(at_k);
           next_v(at_v);
-          vector_phase(is_cached, it);
         }
         pv_part(is_cached, at_v);
         next_v(at_v);
       };
-      const int mid = min(max(vis.n_cached, v0), v1);
+      const int mid = min(max(item.n_cached, v0), v1);
       if (v0 < mid) run_tiles(kCached, v0, mid);
       if (mid < v1) run_tiles(kNew, mid, v1);
 
@@ -821,14 +902,13 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       for (int w = 0; w < ROWS / 32; ++w) any |= flags[w];
       again = again || __builtin_amdgcn_readfirstlane(any);
     } else {
-      const int my_h = g * a.gs + my_r % a.gs;
-      const uint16_t* qp = static_cast<const uint16_t*>(a.q) + sb * a.q_sb + (tok0 + my_t) * a.q_st + my_h * a.q_sh;
+      const uint16_t* qp = static_cast<const uint16_t*>(a.q) + q_at;
 #pragma unroll
       for (int s = 0; s < kKSteps; ++s) qreg[s] = __builtin_bit_cast(bf16x8, ld16(qp + 8 * h2 + 16 * s));
 #pragma unroll 1
       for (int it = v0; it < v1; ++it) {
-        const bool of_cache = it < vis.n_cached;
-        const int kb = vis.tile(it) * kBN;
+        const bool of_cache = it < item.n_cached;
+        const int kb = item.tile(it) * kBN;
         __syncthreads();
         if (of_cache) issue_cached(0, 0, entry_of(it));
         else issue_new(it, 0, 0);
@@ -836,7 +916,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         clean(it, 0);
         __syncthreads();
         uint32_t pages = 0;  // the tile's pages that are none
-        if (of_cache && table)
+        if (of_cache && !str)
           for (int i = 0; i < kBN / kPage; ++i) {
             const int e = table[min(kb / kPage + i, last_page)];
             if (e < 0 || e >= end_page) pages |= 1u << i;
@@ -880,8 +960,8 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     const float l_tot = xor32_sum(l_run);
     if (whole) {
       const float inv = 1.f / l_tot;
-      if (row0 + wave * 32 + l32 < n_rows) {
-        const int64_t at = sb * a.o_sb + (tok0 + my_t) * a.o_st + (int64_t)(g * a.gs + my_r % a.gs) * a.o_sh;
+      if (item.row0 + wave * 32 + l32 < n_rows) {
+        const int64_t at = item.o_off + my_t * a.o_st + (my_r - my_t * a.gs) * a.o_sh;
 #pragma unroll
         for (int mb = 0; mb < kMBlocks; ++mb)
 #pragma unroll
@@ -909,32 +989,40 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       }
     }
   }
+  return again;
+}
+
+// The careful loop is a function of its own (with the arguments from memory): inlined, it
+// would take registers from the fast one.
+template <int D, int ROWS, int PARTS>
+__device__ __attribute__((noinline)) void extend_again(const ExtendArgs* a, TileRing<D, ROWS>* ring) {
+  extend_range<D, ROWS, PARTS, true>(*a, *ring);
 }
 
 template <int D, int ROWS, int PARTS>
 __global__ __launch_bounds__(2 * ROWS, (TileShape<D, ROWS>::kWavesPerSimd)) void extend_tile_kernel(ExtendArgs a) {
   __shared__ __align__(1024) TileRing<D, ROWS> ring;
-  if (extend_range<D, ROWS, PARTS, false>(a, ring)) extend_range<D, ROWS, PARTS, true>(a, ring);
+  if (extend_range<D, ROWS, PARTS, false>(a, ring)) extend_again<D, ROWS, PARTS>(a.copy, &ring);
 }
 
 // ---------------------------------------------------------------------------
 // Items that several workgroups share: one row a wave, its lanes over groups of partials
 // and the dimensions.  The workgroups' x is the range that an item starts in.
-template <int D, int ROWS, int TILE>
+template <int D, int ROWS>
 __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
   constexpr int kLanes = D / 4, kGroups = kWave / kLanes;
   const int lane = threadIdx.x & 63;
   const int row = blockIdx.y * 4 + (threadIdx.x >> 6);
-  const ExtendPlan plan = extend_plan<ROWS, TILE>(a);
+  const ExtendHead head = scalar_load(a.head);
   const int rng = blockIdx.x;
-  if (rng + 1 >= plan.used) return;
-  const int64_t g0 = rng * plan.range, g1 = g0 + plan.range;
-  const ExtendItem item = extend_item(plan, g1 - 1, a.n_ret, a.n_str);
-  if (item.first < g0 || item.first + item.places <= g1) return;  // starts before this range, or ends in it
-  const ExtendSeq seq = extend_seq(a, item.b);
-  const int r = item.rb * ROWS + row;
-  if (r >= seq.n * a.gs) return;
-  const int last = (int)((item.first + item.places - 1) / plan.range);
+  if (rng + 1 >= head.used) return;
+  // the item that goes on behind the range's end
+  const int64_t g0 = rng * head.range, g1 = g0 + head.range;
+  const ExtendItem item = scalar_load(a.items + scalar_load(a.first_item + rng + 1));
+  if (item.first < g0 || item.first >= g1) return;  // starts before this range, or behind it
+  const int r = item.row0 + row;
+  if (r >= item.n_new * a.gs) return;
+  const int last = (int)div64(item.first + item.places - 1, head.range);
   auto slot = [&](int w) { return (int64_t)(2 * w + (w == rng ? 1 : 0)) * ROWS + row; };
   // a partial without a key has m = -inf and l = 0 (keys with NaN scores leave a NaN sum)
   float M = -INFINITY;
@@ -961,13 +1049,11 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
     for (int e = 0; e < 4; ++e) o[e] = wave_xor_sum(o[e], i);
   }
   if (lane >= kLanes) return;
-  const int g = a.kv_heads[item.str ? a.n_ret + item.kvl : item.kvl];
-  const int64_t sb = a.cu_seqlens ? 0 : item.b, tok0 = a.cu_seqlens ? seq.row0 : 0;
-  const int t = r / a.gs, h = g * a.gs + r % a.gs;
   const float inv = 1.f / L;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] *= inv;
-  const int64_t at = sb * a.o_sb + (tok0 + t) * a.o_st + h * a.o_sh + 4 * lane;
+  const int t = div_gs(a, r);
+  const int64_t at = item.o_off + t * a.o_st + (r - t * a.gs) * a.o_sh + 4 * lane;
   if (a.out_f32) store4<true>(a, at, o);
   else store4<false>(a, at, o);
 }
@@ -978,18 +1064,29 @@ static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
   a.min_tiles = 2;
   a.part_acc = static_cast<float*>(a.workspace);
   a.part_ml = a.part_acc + (int64_t)2 * a.wgs * ROWS * D;
+  a.head = reinterpret_cast<ExtendHead*>(a.part_ml + (int64_t)2 * a.wgs * ROWS * 2);
+  a.copy = reinterpret_cast<ExtendArgs*>(a.head + 1);
+  a.items = reinterpret_cast<ExtendItem*>(a.copy + 1);
+  const int64_t rows = (a.cu_seqlens ? std::min<int64_t>(a.total, (int64_t)a.B * a.T) : (int64_t)a.B * a.T) * a.gs;
+  const int64_t n_items = (a.n_ret + a.n_str) * (rows / ROWS + a.B);  // at most
+  a.first_item = reinterpret_cast<int32_t*>(a.items + n_items);
+  const int plan_wgs = (int)std::min<int64_t>((n_items + 255) / 256, a.cus);
+  hipLaunchKernelGGL((extend_plan_kernel<ROWS, kBN>), dim3(plan_wgs), dim3(256), 0, s, a);
+  if (hipError_t e = hipGetLastError()) return e;
   const dim3 grid((a.wgs + 7) / 8 * 8);
   if (a.out_f32) hipLaunchKernelGGL((extend_tile_kernel<D, ROWS, 3>), grid, dim3(2 * ROWS), 0, s, a);
   else hipLaunchKernelGGL((extend_tile_kernel<D, ROWS, 1>), grid, dim3(2 * ROWS), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL((extend_merge_kernel<D, ROWS, kBN>), dim3(a.wgs - 1, ROWS / 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((extend_merge_kernel<D, ROWS>), dim3(a.wgs - 1, ROWS / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-// Bytes of the partials of the largest launch: two blocks of rows a workgroup.
-size_t extend_workspace(int d, int cus) {
+// Bytes of the partials of the largest launch (two blocks of rows a workgroup), and of the
+// plan of so many tokens in so many sequences.
+size_t extend_workspace(int64_t batch, int64_t tokens, int hq, int hkv, int d, int cus) {
   const size_t rows = d == 64 ? 128 * 3 : 256;
-  return (size_t)2 * cus * rows * (d + 2) * sizeof(float);
+  const size_t items = (size_t)hkv * (tokens * (hq / hkv) / 128 + batch);
+  return (size_t)2 * cus * rows * (d + 2) * sizeof(float) + sizeof(ExtendHead) + sizeof(ExtendArgs) + items * sizeof(ExtendItem) + 3 * cus * sizeof(int32_t);
 }
 
 hipError_t launch_extend(const ExtendArgs& a, int dtype, int d, hipStream_t s) {
