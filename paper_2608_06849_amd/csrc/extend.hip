@@ -461,9 +461,7 @@ struct TileShape {
   static constexpr int kAhead = kPair ? 3 : 2;
   static constexpr int kKSlots = kPair ? 4 : D == 128 ? 2 : 3;
   static constexpr int kVSlots = kPair ? 4 : 3;
-  static constexpr int kWavesPerSimd = D == 64 ? 3 : 2;
   static constexpr int kLoads = kBN * (D / 8) / kThreads;  // loads per thread and tile, K or V
-  static constexpr int kWgsPerCu = kPair ? 1 : D == 64 ? 3 : 2;
 };
 
 template <int D, int ROWS>
@@ -542,18 +540,18 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
   }
   const int dim0 = (32 * Shape::kLoads * wave + (lane >> 1)) % D, half0 = (lane & 1) ^ ((dim0 >> 3) & 1);
   const uint32_t dma_v = 2u * (dim0 * kPage + 8 * half0);
-  auto k_operand = [&](uint32_t at, int s, int blk) __attribute__((always_inline)) {
+  auto k_operand = [&](uint32_t at, int blk) __attribute__((always_inline)) {
     typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
-    return *reinterpret_cast<lds_bf16x8*>((at ^ (32u * s)) + 64u * D * blk);
+    return *reinterpret_cast<lds_bf16x8*>(at + 64u * D * blk);
   };
   // cached: a tile of pages, else of new rows
-  auto v_operand = [&](auto cached, uint32_t at, int ks, int mb) __attribute__((always_inline)) {
+  auto v_operand = [&](auto cached, uint32_t at, int ks) __attribute__((always_inline)) {
     if constexpr (decltype(cached)::value) {
       typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
-      return *reinterpret_cast<lds_bf16x8*>(at + 32u * D * ks + 1024u * mb);
+      return *reinterpret_cast<lds_bf16x8*>(at + 32u * D * ks);
     } else {
       typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-      const uint32_t x = (at ^ (64u * mb)) + 32u * D * ks;
+      const uint32_t x = at + 32u * D * ks;
       const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4*>(x));
       const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_i16x4*>(x + 8u * D));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -602,19 +600,23 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     const int64_t unit0 = str ? item.ring : item.rank;
     const uint16_t* kc = static_cast<const uint16_t*>(str ? a.rk : a.pk) + unit0 * (kPage * D);
     const uint16_t* vc = static_cast<const uint16_t*>(str ? a.rv : a.pv) + unit0 * (kPage * D);
-    const int32_t* table = a.block_table + item.table;
+    const int32_t* item_table = a.block_table + item.table;
     const int last_page = max(div_up(cached, kPage) - 1, 0);
     const int end_page = str ? a.ring_blocks : a.num_pages;
     int64_t k_st = a.k_st, v_st = a.v_st;
     int n_sink = a.n_sink, window = a.window;
     // registers of their own, not those of the argument block's load
     if constexpr (!CAREFUL) asm("" : "+s"(k_st), "+s"(v_st), "+s"(n_sink), "+s"(window));
+    // new tiles: byte offsets from the tile's first row, where they fit 32 bits
+    const bool near = k_st < (1 << 24) && v_st < (1 << 24);
+    uint32_t new_k[Shape::kLoads], new_v[Shape::kLoads];
+#pragma unroll
+    for (int jj = 0; jj < Shape::kLoads; ++jj) {
+      const int r = kBlockRows * (Shape::kLoads * wave + jj) + lane / Tile::kChunks, pc = lane % Tile::kChunks;
+      new_k[jj] = 2u * ((uint32_t)r * (uint32_t)k_st + 8 * (pc ^ Tile::kx(r)));
+      new_v[jj] = 2u * ((uint32_t)r * (uint32_t)v_st + 8 * (pc ^ Tile::vx(r)));
+    }
     bool bad = false;  // this wave has met a page outside the cache, or a V that the fast loop cannot take
-    // Page of this wave's part of a cached tile: the block table's entry, read ahead of its use.
-    auto entry_of = [&](int it) __attribute__((always_inline)) {
-      const int pg = min(item.tile(it) * (kBN / kPage) + my_page, last_page);
-      return str ? pg : scalar_load(table + pg);
-    };
     auto issue_cached = [&](int slot_k, int slot_v, int entry_v) __attribute__((always_inline)) {
       int entry = uniform(entry_v);
       if (entry < 0 || entry >= end_page) {
@@ -631,12 +633,24 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         lds_dma16_from(vu, dma_v + 1024 * jj, &ring.v[slot_v][512 * j]);
       }
     };
-    auto issue_new = [&](int it, int slot_k, int slot_v) __attribute__((always_inline)) {
-      const int kb = item.tile(it) * kBN;
+    auto issue_new = [&](int kb, int slot_k, int slot_v) __attribute__((always_inline)) {
+      if (kb + kBN <= n_new && near) {
+        const uint16_t* kt = kn + kb * k_st;
+        const uint16_t* vt = vn + kb * v_st;
+#pragma unroll
+        for (int jj = 0; jj < Shape::kLoads; ++jj) {
+          const int j = Shape::kLoads * wave + jj;
+          lds_dma16_from(kt, new_k[jj], &ring.k[slot_k][512 * j]);
+          lds_dma16_from(vt, new_v[jj], &ring.v[slot_v][512 * j]);
+        }
+        return;
+      }
+      int ln = lane;
+      asm volatile("" : "+v"(ln));  // rare: its addresses are not to be kept in registers
 #pragma unroll
       for (int jj = 0; jj < Shape::kLoads; ++jj) {
         const int j = Shape::kLoads * wave + jj;
-        const int r = kBlockRows * j + lane / Tile::kChunks, pc = lane % Tile::kChunks;
+        const int r = kBlockRows * j + ln / Tile::kChunks, pc = ln % Tile::kChunks;
         const int64_t row = min(kb + r, n_new - 1);  // rows behind the last repeat it; no query sees them
         lds_dma16_at(kn + row * k_st + 8 * (pc ^ Tile::kx(r)), &ring.k[slot_k][512 * j]);
         lds_dma16_at(vn + row * v_st + 8 * (pc ^ Tile::vx(r)), &ring.v[slot_v][512 * j]);
@@ -644,19 +658,21 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     };
     // V of a tile that this wave's loads have brought: zeroes tokens behind the cache's last
     // one, and looks for values that are not finite where a row does not see all keys.
-    auto clean = [&](int it, int slot_v) __attribute__((always_inline)) {
-      const int kb = item.tile(it) * kBN;
+    auto clean = [&](int it, int kb, int slot_v) __attribute__((always_inline)) {
       const bool of_cache = it < item.n_cached;
       const bool tail = of_cache && kb + kBN > cached;
       const bool masked = of_cache ? band : kb + kBN - 1 > item.t_first || !(start + kb + kBN - 1 < n_sink || start + kb >= lo_off + item.t_last);
       if (!tail && !masked) return;
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
 #pragma unroll
       for (int jj = 0; jj < Shape::kLoads; ++jj) {
         const int j = Shape::kLoads * wave + jj;
-        u32x4* at = reinterpret_cast<u32x4*>(&ring.v[slot_v][512 * j + 8 * lane]);
+        u32x4* at = reinterpret_cast<u32x4*>(&ring.v[slot_v][512 * j + 8 * ln]);
         u32x4 x = *at;
         if (tail) {
-          const int left = cached - (kb + (32 * j / D) * kPage + 8 * half0);
+          const int half = (ln & 1) ^ ((((32 * j + (ln >> 1)) % D) >> 3) & 1);
+          const int left = cached - (kb + (32 * j / D) * kPage + 8 * half);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = left >= 2 * e + 2 ? x[e] : left == 2 * e + 1 ? x[e] & 0xffffu : 0u;
           *at = x;
@@ -677,71 +693,93 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
     f32x16 sacc[2];           // S^T of the current tile, two 32-key blocks
     bf16x8 pop[PARTS][4];     // P^T operands of the previous tile's 4 key steps
 
-    auto pv_part = [&](auto is_cached, int slot) __attribute__((always_inline)) {
-      const uint32_t at = (decltype(is_cached)::value ? paddr0 : vaddr0) + (uint32_t)slot * Tile::kBytes;
+    // Operands in the order of their products: V^T of each key step and 32-dim block, then K
+    // of each step and block.  They are read kDepth products ahead; the barriers to the
+    // scheduler keep that order (left to it, every product waited for its own read).
+    constexpr int kNV = 4 * kMBlocks, kNK = 2 * kKSteps, kDepth = 6;
+    auto products = [&](auto is_cached, auto with_v, auto with_k, int slot_k, int slot_v) __attribute__((always_inline)) {
+      constexpr int kFirst = decltype(with_v)::value ? 0 : kNV, kLast = decltype(with_k)::value ? kNV + kNK : kNV;
+      uint32_t ka[kKSteps], va[kMBlocks];
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
+      for (int s = 0; s < kKSteps; ++s) ka[s] = (kaddr0 + (uint32_t)slot_k * Tile::kBytes) ^ (32u * s);
 #pragma unroll
-        for (int mb = 0; mb < kMBlocks; ++mb) {
-          const bf16x8 v = v_operand(is_cached, at, ks, mb);
+      for (int mb = 0; mb < kMBlocks; ++mb)
+        va[mb] = decltype(is_cached)::value ? paddr0 + (uint32_t)slot_v * Tile::kBytes + 1024u * mb
+                                            : (vaddr0 + (uint32_t)slot_v * Tile::kBytes) ^ (64u * mb);
+      bf16x8 op[kDepth];
+      auto read = [&](int o) __attribute__((always_inline)) {
+        op[o % kDepth] = o < kNV ? v_operand(is_cached, va[o % kMBlocks], o / kMBlocks) : k_operand(ka[(o - kNV) / 2], o & 1);
+      };
 #pragma unroll
-          for (int i = PARTS - 1; i >= 0; --i) acc_o[mb] = mfma32(v, pop[i][ks], acc_o[mb]);
+      for (int o = kFirst; o < kFirst + kDepth; ++o) read(o);
+      if constexpr (decltype(with_k)::value) {
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sacc[blk][i] = 0.f;
+      }
+#pragma unroll
+      for (int o = kFirst; o < kLast; ++o) {
+        __builtin_amdgcn_sched_barrier(0);
+        const bf16x8 x = op[o % kDepth];
+        if (o < kNV) {
+#pragma unroll
+          for (int i = PARTS - 1; i >= 0; --i) acc_o[o % kMBlocks] = mfma32(x, pop[i][o / kMBlocks], acc_o[o % kMBlocks]);
+        } else {
+          sacc[o & 1] = mfma32(x, qreg[(o - kNV) / 2], sacc[o & 1]);
         }
+        if (o + kDepth < kLast) read(o + kDepth);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     };
-    auto qk_part = [&](int slot) __attribute__((always_inline)) {
-      const uint32_t at = kaddr0 + (uint32_t)slot * Tile::kBytes;
-#pragma unroll
-      for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sacc[blk][i] = 0.f;
-#pragma unroll
-      for (int s = 0; s < kKSteps; ++s)
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) sacc[blk] = mfma32(k_operand(at, s, blk), qreg[s], sacc[blk]);
-    };
-    // Steady-state MFMA phase, at raised wave priority: operands are read a few MFMAs ahead
-    // of their products.
+    constexpr std::integral_constant<bool, true> kYes{};
+    constexpr std::integral_constant<bool, false> kNo{};
+    auto pv_part = [&](auto is_cached, int slot) __attribute__((always_inline)) { products(is_cached, kYes, kNo, 0, slot); };
+    auto qk_part = [&](int slot) __attribute__((always_inline)) { products(kCached, kNo, kYes, slot, 0); };
+    // Steady-state MFMA phase, at raised wave priority.
     auto mfma_phase = [&](auto is_cached, int slot_k, int slot_v) __attribute__((always_inline)) {
       __builtin_amdgcn_s_setprio(1);
-      pv_part(is_cached, slot_v);
-      qk_part(slot_k);
-      constexpr int kReads = decltype(is_cached)::value ? 1 : 2;  // LDS reads of a V^T operand
-      __builtin_amdgcn_sched_group_barrier(0x100, 4 * kReads, 0);
-#pragma unroll
-      for (int i = 0; i < D / 8 - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, PARTS, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, PARTS, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < D / 8 - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-      __builtin_amdgcn_sched_barrier(0);
+      products(is_cached, kYes, kYes, slot_k, slot_v);
       __builtin_amdgcn_s_setprio(0);
     };
 
-    // Key (place within the tile) of score i of block blk.
-    auto key_of = [&](int blk, int i) __attribute__((always_inline)) { return 32 * blk + 16 * (i >> 3) + 8 * h2 + (i & 7); };
-    // Whether this lane's row sees key j (position, slot, or new token).
-    auto sees = [&](bool of_cache, int j) __attribute__((always_inline)) {
-      if (of_cache) {
-        const int r = j - n_sink;
-        return (j < cached) & ((r < 0) | (item.rbase + r - (r > item.rrem ? window : 0) >= lo_off + my_t));
+    // Whether this lane's row sees a key: with c the key's place in its run of 8 h2 .. (a
+    // constant where it is used), comparisons with a few limits of the tile, of which a
+    // register each is enough.
+    struct Limits { int end, sinks, from, wrap, from2; };
+    auto limits_of = [&](bool of_cache, int kb) __attribute__((always_inline)) {
+      const int at = kb + 8 * h2;
+      Limits x;
+      if (of_cache) {  // c < end and (c < sinks or from <= c <= wrap or c >= from2)
+        x.end = cached - at;
+        x.sinks = n_sink - at;
+        x.from = lo_off + my_t - item.rbase + n_sink - at;
+        x.wrap = item.rrem + n_sink - at;
+        x.from2 = x.from + window;
+        if (!str) x.sinks = x.end;
+      } else {  // c <= my_t and (c < sinks or c >= from)
+        x.end = my_t + 1 - at;
+        x.sinks = n_sink - start - at;
+        x.from = lo_off + my_t - start - at;
+        x.wrap = INT32_MAX;
+        x.from2 = x.from;
       }
-      return (j <= my_t) & ((start + j < n_sink) | (start + j >= lo_off + my_t));
+      return x;
     };
-    auto apply_mask = [&](bool of_cache, int kb) __attribute__((always_inline)) {
+    // c of score i of block blk
+    auto place_of = [&](int blk, int i) __attribute__((always_inline)) { return 32 * blk + 16 * (i >> 3) + (i & 7); };
+    auto sees = [&](auto of_cache, const Limits& x, int c) __attribute__((always_inline)) {
+      if constexpr (decltype(of_cache)::value)
+        return (c < x.end) & ((c < x.sinks) | ((c >= x.from) & (c <= x.wrap)) | (c >= x.from2));
+      else
+        return (c < x.end) & ((c < x.sinks) | (c >= x.from));
+    };
+    auto apply_mask = [&](auto of_cache, int kb) __attribute__((always_inline)) {
+      const Limits x = limits_of(decltype(of_cache)::value, kb);
 #pragma unroll
       for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sacc[blk][i] = sees(of_cache, kb + key_of(blk, i)) ? sacc[blk][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) sacc[blk][i] = sees(of_cache, x, place_of(blk, i)) ? sacc[blk][i] : -INFINITY;
     };
     // Exponentials against m_use into the P^T operands; their sum.
     auto exps = [&]() __attribute__((always_inline)) {
@@ -795,9 +833,8 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
 
     barrier();  // the ring's last use (the range's previous item) is over
     if constexpr (!CAREFUL) {
-      auto valu_phase = [&](auto is_cached, int it) __attribute__((always_inline)) {
+      auto valu_phase = [&](auto is_cached, int kb) __attribute__((always_inline)) {
         constexpr bool of_cache = decltype(is_cached)::value;
-        const int kb = item.tile(it) * kBN;
         bool dead = false, mask;
         if constexpr (of_cache) {
           mask = kb + kBN > cached || band;
@@ -814,23 +851,41 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
               for (int e = 0; e < 8; ++e) pop[i][ks][e] = (bf16)0.f;
           return;
         }
-        if (mask) apply_mask(of_cache, kb);
+        if (mask) apply_mask(is_cached, kb);
         softmax_tile();
       };
       // Slots of the tile that is loaded next, of the tile whose K and of the one whose V is
       // read next.
       int in_k = 0, in_v = 0, at_k = 0, at_v = 0;
+      asm("" : "+s"(at_k));  // not known to be 0: no addresses of slot 0 are kept
       auto next_k = [&](int& x) __attribute__((always_inline)) { x = x + 1 == Shape::kKSlots ? 0 : x + 1; };
       auto next_v = [&](int& x) __attribute__((always_inline)) { x = x + 1 == Shape::kVSlots ? 0 : x + 1; };
-      int entry = 0;  // of the next tile that is loaded, if it is cached
-      auto issue = [&](int it) __attribute__((always_inline)) {
-        if (it < item.n_cached) issue_cached(in_k, in_v, entry);
-        else issue_new(it, in_k, in_v);
+      // First keys of the current tile and of the next ones, up to the one that is loaded next.
+      int kbs[Shape::kAhead + 1];
+#pragma unroll
+      for (int u = 0; u <= Shape::kAhead; ++u) kbs[u] = item.tile(v0 + u) * kBN;
+      // Block table entries of this wave's page in 64 tiles, one a lane: a load waits for the
+      // direct loads before it, and a scalar one would make every LDS read behind it wait for
+      // all of them.
+      int entries = 0, entries0 = 0;
+      auto read_entries = [&](int it) __attribute__((always_inline)) {
+        entries0 = it;
+        entries = item_table[min((it + lane) * (kBN / kPage) + my_page, last_page)];
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);  // here, not at every use
+      };
+      auto issue = [&](int it, int kb) __attribute__((always_inline)) {
+        if (it < item.n_cached) {
+          int page = min(kb / kPage + my_page, last_page);
+          if (!str) {
+            if (it - entries0 == kWave) read_entries(it);
+            page = __builtin_amdgcn_readlane(entries, it - entries0);
+          }
+          issue_cached(in_k, in_v, page);
+        } else {
+          issue_new(kb, in_k, in_v);
+        }
         next_k(in_k);
         next_v(in_v);
-      };
-      auto read_entry = [&](int it) __attribute__((always_inline)) {
-        if (it < item.n_cached && it < v1) entry = entry_of(it);
       };
       // The barrier of a tile follows each wave's wait for its loads of the next one (with
       // loads three tiles ahead those of the one after may stay in flight); after it, the
@@ -841,49 +896,49 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         if (it + 1 < v1) {
           int s = in_v - (Shape::kAhead - 1);  // the next tile's slot
           if (it + Shape::kAhead > v1) s += it + Shape::kAhead - v1;
-          clean(it + 1, s < 0 ? s + Shape::kVSlots : s);
+          clean(it + 1, kbs[1], s < 0 ? s + Shape::kVSlots : s);
         }
         __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
         barrier();
-        if (it + Shape::kAhead < v1) issue(it + Shape::kAhead);
+        if (it + Shape::kAhead < v1) issue(it + Shape::kAhead, kbs[Shape::kAhead]);
       };
 
       // Prologue: the first tiles and this wave's Q rows, then everything complete.
-      for (int u = 0; u < Shape::kAhead && v0 + u < v1; ++u) {
-        read_entry(v0 + u);
-        issue(v0 + u);
-      }
+      if (!str && v0 < item.n_cached) read_entries(v0);
+#pragma unroll
+      for (int u = 0; u < Shape::kAhead; ++u)
+        if (v0 + u < v1) issue(v0 + u, kbs[u]);
       {
         const uint16_t* qp = static_cast<const uint16_t*>(a.q) + q_at;
 #pragma unroll
         for (int s = 0; s < kKSteps; ++s) qreg[s] = __builtin_bit_cast(bf16x8, ld16(qp + 8 * h2 + 16 * s));
       }
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
-      clean(v0, 0);
-      if (grp == 1) read_entry(v0 + Shape::kAhead);
+      clean(v0, kbs[0], 0);
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       barrier();
 
       // Every wave runs MFMA, vector phase, MFMA, ..: waves 0-3 take the barrier of a tile
-      // after its vector phase, waves 4-7 after its MFMA phase.  A block table entry is read
-      // while the vector phase runs.
+      // after its vector phase, waves 4-7 after its MFMA phase.
       auto vector_phase = [&](auto is_cached, int it) __attribute__((always_inline)) {
         if (grp == 1) sync_tile(it);
-        read_entry(it + grp + Shape::kAhead);
-        valu_phase(is_cached, it);
-        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+        valu_phase(is_cached, kbs[0]);
         if (grp == 0) sync_tile(it);
+        const int kb_next = item.tile(it + 1 + Shape::kAhead) * kBN;
+#pragma unroll
+        for (int u = 0; u < Shape::kAhead; ++u) kbs[u] = kbs[u + 1];
+        kbs[Shape::kAhead] = kb_next;
       };
       auto run_tiles = [&](auto is_cached, int i0, int i1) __attribute__((always_inline)) {
         qk_part(at_k);
         next_k(at_k);
+        vector_phase(is_cached, i0);
 #pragma unroll 1
-        for (int it = i0;;) {
-          vector_phase(is_cached, it);
-          if (++it == i1) break;
+        for (int it = i0 + 1; it < i1; ++it) {
           mfma_phase(is_cached, at_k, at_v);
           next_k(at_k);
           next_v(at_v);
+          vector_phase(is_cached, it);
         }
         pv_part(is_cached, at_v);
         next_v(at_v);
@@ -910,23 +965,27 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         const bool of_cache = it < item.n_cached;
         const int kb = item.tile(it) * kBN;
         __syncthreads();
-        if (of_cache) issue_cached(0, 0, entry_of(it));
-        else issue_new(it, 0, 0);
+        const int page = min(kb / kPage + my_page, last_page);
+        if (of_cache) issue_cached(0, 0, str ? page : item_table[page]);
+        else issue_new(kb, 0, 0);
         __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        clean(it, 0);
+        clean(it, kb, 0);
         __syncthreads();
         uint32_t pages = 0;  // the tile's pages that are none
         if (of_cache && !str)
           for (int i = 0; i < kBN / kPage; ++i) {
-            const int e = table[min(kb / kPage + i, last_page)];
+            const int e = item_table[min(kb / kPage + i, last_page)];
             if (e < 0 || e >= end_page) pages |= 1u << i;
           }
-        auto seen = [&](int j) __attribute__((always_inline)) { return sees(of_cache, kb + j) && !((pages >> (j / kPage)) & 1u); };
+        const Limits x = limits_of(of_cache, kb);
+        auto seen = [&](int c) __attribute__((always_inline)) {
+          return (of_cache ? sees(kCached, x, c) : sees(kNew, x, c)) && !((pages >> ((c + 8 * h2) / kPage)) & 1u);
+        };
         qk_part(0);
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sacc[blk][i] = seen(key_of(blk, i)) ? sacc[blk][i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) sacc[blk][i] = seen(place_of(blk, i)) ? sacc[blk][i] : -INFINITY;
         softmax_tile();
         // P.V with the finite values, and NaN where a row sees one that is not
 #pragma unroll
@@ -936,7 +995,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
           for (int i = 0; i < 16; ++i) hits[i] = 0.f;
 #pragma unroll
           for (int ks = 0; ks < 4; ++ks) {
-            const bf16x8 v = of_cache ? v_operand(kCached, paddr0, ks, mb) : v_operand(kNew, vaddr0, ks, mb);
+            const bf16x8 v = of_cache ? v_operand(kCached, paddr0 + 1024u * mb, ks) : v_operand(kNew, vaddr0 ^ (64u * mb), ks);
             const i16x8 bits = __builtin_bit_cast(i16x8, v);
             i16x8 fin;
             bf16x8 ind, on;
@@ -945,7 +1004,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
               const bool out = (bits[e] & 0x7f80) == 0x7f80;
               fin[e] = out ? (short)0 : bits[e];
               ind[e] = (bf16)(out ? 1.f : 0.f);
-              on[e] = (bf16)(seen(16 * ks + 8 * h2 + e) ? 1.f : 0.f);
+              on[e] = (bf16)(seen(16 * ks + e) ? 1.f : 0.f);
             }
 #pragma unroll
             for (int i = PARTS - 1; i >= 0; --i) acc_o[mb] = mfma32(__builtin_bit_cast(bf16x8, fin), pop[i][ks], acc_o[mb]);
@@ -1000,7 +1059,7 @@ __device__ __attribute__((noinline)) void extend_again(const ExtendArgs* a, Tile
 }
 
 template <int D, int ROWS, int PARTS>
-__global__ __launch_bounds__(2 * ROWS, (TileShape<D, ROWS>::kWavesPerSimd)) void extend_tile_kernel(ExtendArgs a) {
+__global__ __launch_bounds__(2 * ROWS, (D == 64 && PARTS == 1 ? 3 : 2)) void extend_tile_kernel(ExtendArgs a) {
   __shared__ __align__(1024) TileRing<D, ROWS> ring;
   if (extend_range<D, ROWS, PARTS, false>(a, ring)) extend_again<D, ROWS, PARTS>(a.copy, &ring);
 }
@@ -1060,7 +1119,7 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
 
 template <int D, int ROWS>
 static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
-  a.wgs = a.cus * TileShape<D, ROWS>::kWgsPerCu;
+  a.wgs = a.cus * (ROWS == 256 ? 1 : D == 64 && !a.out_f32 ? 3 : 2);
   a.min_tiles = 2;
   a.part_acc = static_cast<float*>(a.workspace);
   a.part_ml = a.part_acc + (int64_t)2 * a.wgs * ROWS * D;
