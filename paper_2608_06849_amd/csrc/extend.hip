@@ -49,12 +49,11 @@ __device__ __forceinline__ int ring_position(int c, int start, int n_sink, int w
 
 // ---------------------------------------------------------------------------
 // The work space.  An item's places: kUnit for each tile that its rows visit, about (a
-// first number and a step from one block of rows to the next), and kItemCost tiles for its
+// first number and a step from one block of rows to the next), and item_cost tiles for its
 // start.  A range of places stands for the same share of the item's visits, so the numbers
 // need not be exact.  A first launch writes the items and where every range starts, so that
 // the others begin with a few scalar loads.
 constexpr int kUnit = 16;
-constexpr int kItemCost = 3;
 constexpr int kPlanSeqs = 1024;  // sequences of a launch; larger batches go in parts
 
 struct ExtendHead {
@@ -130,16 +129,14 @@ template <int ROWS, int TILE>
 __device__ __forceinline__ SeqCost seq_cost(const ExtendArgs& a, const ExtendSeq& s) {
   SeqCost x;
   x.blocks = (int)(((int64_t)s.n * a.gs + ROWS - 1) / ROWS);
-  const int step = max(1, kUnit * ROWS / (TILE * a.gs));  // new tiles that the next block of rows sees more
-  const int n_new = div_up(s.n, TILE), first = div_up(div_up(ROWS, a.gs), TILE);
+  const int n_new = div_up(s.n, TILE);
   const int paged = div_up(min(s.start, a.max_pages * kPage), TILE);
   const int ring = div_up(min(s.start, a.ring_cap), TILE);
-  x.a[0] = (int64_t)kUnit * (kItemCost + paged + min(n_new, first));
-  x.c[0] = step;
-  // the band of a block has at most window + tokens of the block keys
-  const int band = div_up(a.n_sink, TILE) + div_up(a.window, TILE) + first + 1;
-  x.a[1] = (int64_t)kUnit * (kItemCost + (a.evict ? ring + min(n_new, first) : min(ring + n_new, band)));
-  x.c[1] = a.evict ? step : 0;
+  x.a[0] = (int64_t)kUnit * (a.item_cost + paged + min(n_new, a.block_tiles));
+  x.c[0] = a.block_step;
+  // masked tiles of rings and windows take half as long again
+  x.a[1] = (int64_t)kUnit * a.item_cost + (kUnit * 3 / 2) * (int64_t)(a.evict ? ring + min(n_new, a.block_tiles) : min(ring + n_new, a.band_tiles));
+  x.c[1] = a.evict ? a.block_step : 0;
   return x;
 }
 
@@ -165,16 +162,17 @@ __device__ __forceinline__ void set_visits(const ExtendArgs& a, ExtendItem& x) {
   const int sinks = div_up(min(a.n_sink, x.cached), TILE);
   int f1 = sinks, l1 = sinks, f2 = 0, l2 = 0;  // runs of window tiles
   if (w0 < start) {
-    const int p = a.n_sink + (w0 - a.n_sink) % a.window, q = a.n_sink + (start - 1 - a.n_sink) % a.window;
-    if (start - w0 >= a.window) {
+    const int back = start - 1 - w0;  // from the newest token's slot, offset rrem, to the oldest visible one's
+    const int q = a.n_sink + x.rrem, p = a.n_sink + x.rrem - back;
+    if (back + 1 >= a.window) {
       l1 = all;
-    } else if (p <= q) {
+    } else if (back <= x.rrem) {
       f1 = max(sinks, p / TILE);
       l1 = q / TILE + 1;
     } else {
       f1 = max(sinks, a.n_sink / TILE);
       l1 = q / TILE + 1;
-      f2 = max(max(f1, l1), p / TILE);
+      f2 = max(max(f1, l1), (p + a.window) / TILE);
       l2 = all;
     }
   }
@@ -196,6 +194,7 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
   __shared__ int64_t s_places[2][kPlanSeqs + 1];
   __shared__ int s_blocks[kPlanSeqs + 1];
   __shared__ int64_t s_wave[3][4];
+  __shared__ int64_t s_first[256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n_kv[2] = {a.n_ret, a.n_str};
   int64_t x[3][4], sum[3] = {0, 0, 0};
@@ -248,6 +247,7 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
     *a.head = ExtendHead{total, range, used, n_items};
     *a.copy = a;
   }
+  const bool few = n_items <= 256;  // one item a thread of the first workgroup
   for (int idx = blockIdx.x * 256 + tid; idx < n_items; idx += gridDim.x * 256) {
     ExtendItem it;
     it.str = idx >= n_kv[0] * blocks;
@@ -283,8 +283,25 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
     it.t_last = div_gs(a, min(it.row0 + ROWS, s.n * a.gs) - 1);
     set_visits<TILE>(a, it);
     a.items[idx] = it;
+    if (few) {
+      s_first[tid] = it.first;
+      continue;
+    }
     // ranges that start in this item
-    for (int w = (int)div64(it.first + range - 1, range); w < used && w * range < it.first + it.places; ++w) a.first_item[w] = idx;
+    const int w1 = min(used - 1, (int)div64(it.first + it.places - 1, range));
+    for (int w = (int)div64(it.first + range - 1, range); w <= w1; ++w) a.first_item[w] = idx;
+  }
+  // few items have many ranges each, and each range looks for its item
+  if (!few || blockIdx.x != 0) return;
+  __syncthreads();
+  for (int w = tid; w < used; w += 256) {
+    int i = 0;  // the last item that begins at or before the range
+    for (int hi = n_items; hi - i > 1;) {
+      const int mid = (i + hi) >> 1;
+      if (s_first[mid] <= w * range) i = mid;
+      else hi = mid;
+    }
+    a.first_item[w] = i;
   }
 }
 
@@ -1090,16 +1107,16 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
   for (int i = 1; i < kWave; i *= 2) M = wave_xor_max(M, i);
   float L = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
   for (int w = rng + lane / kLanes; w <= last; w += kGroups) {
     const int64_t at = slot(w);
     const float m = a.part_ml[at * 2], l = a.part_ml[at * 2 + 1];
-    const float f = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : fast_exp2(m - M);
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (m != -INFINITY || l != 0.f) x = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + 4 * (lane % kLanes));
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + 4 * (lane % kLanes));
+    const bool none = m == -INFINITY && l == 0.f;
+    const float f = none ? 0.f : m == -INFINITY ? 1.f : fast_exp2(m - M);
     L += f * l;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+    for (int e = 0; e < 4; ++e) o[e] += none ? 0.f : f * x[e];
   }
 #pragma unroll
   for (int i = kLanes; i < kWave; i *= 2) {
@@ -1121,6 +1138,11 @@ template <int D, int ROWS>
 static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
   a.wgs = a.cus * (ROWS == 256 ? 1 : D == 64 && !a.out_f32 ? 3 : 2);
   a.min_tiles = 2;
+  // an item's start costs as much as so many tiles (its first loads, its stores)
+  a.item_cost = ROWS == 256 ? 12 : 8;
+  a.block_step = std::max(1, kUnit * ROWS / (kBN * a.gs));
+  a.block_tiles = ((ROWS + a.gs - 1) / a.gs + kBN - 1) / kBN;
+  a.band_tiles = (a.n_sink + kBN - 1) / kBN + (a.window + kBN - 1) / kBN + a.block_tiles + 1;
   a.part_acc = static_cast<float*>(a.workspace);
   a.part_ml = a.part_acc + (int64_t)2 * a.wgs * ROWS * D;
   a.head = reinterpret_cast<ExtendHead*>(a.part_ml + (int64_t)2 * a.wgs * ROWS * 2);
