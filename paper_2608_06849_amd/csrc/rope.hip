@@ -12,11 +12,15 @@
 // A workgroup takes up to 16 tokens (appends: those of one 16-position block, so of one
 // page) and a range of heads.  The tokens' cosines and sines are computed once into LDS;
 // a thread keeps one token and one 16-byte piece of its rows, so it reads its pairs'
-// values once and then goes over the heads.  The partners of a half-split pair meet in
-// LDS within the wave.  Values of several tokens pass through an LDS tile into the
+// values once and then goes over the heads, with the rows of the next two on their way.
+// The partners of a half-split pair meet in LDS within the wave.  Values of several tokens pass through an LDS tile into the
 // dimension-major V pages, single tokens are stored from the row.
-// Bound: memory, for single tokens the chain positions -> angles -> stores.
+// Bound: memory, for single tokens the chain positions -> angles -> stores.  Measured: norms
+// and rotation of 8192 tokens (40 heads of 128, bf16) 39 us, 4.3 TB/s; 16 packed prompts
+// of 64 to 2900 tokens (48 heads) into caches 137 us, 3.8 TB/s (191 us with one row on its way and three
+// waves a SIMD); one token of 64 sequences 10 us.
 #include <algorithm>
+#include <type_traits>
 
 #include "aoh_device.h"
 #include "aoh_internal.h"
@@ -48,14 +52,33 @@ __device__ __forceinline__ float2 turn(int64_t p, float f, float scale) {
   }
 }
 
+// Sum over LANES consecutive lanes, the same in each: within 16 by the data-parallel moves
+// (neighbours, pairs, mirrored halves and rows), which need no LDS.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+  x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xF, 0xF, true));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4E, 0xF, 0xF, true));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x141, 0xF, 0xF, true));
+  if (LANES >= 16) x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x140, 0xF, 0xF, true));
+  if (LANES >= 32) x = wave_xor_sum(x, 16);
+  return x;
+}
+
+// Two values as bf16, the first in the low half.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
 template <int D, typename T, bool APPEND>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+__global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
   constexpr int kVec = 16 / sizeof(T);       // values of a thread's piece of a row
   constexpr int kLanes = D / kVec;           // threads of a row
   constexpr int kSlots = 256 / kLanes;       // rows at a time
   constexpr int kToks = kSlots < kPage ? kSlots : kPage;
   __shared__ __align__(16) float2 s_cs[kPage][D / 2];
-  __shared__ __align__(16) float s_y[256][kVec];
+  __shared__ __align__(16) float s_y[256 * kVec + 4];  // and four zeros
   __shared__ __align__(16) T s_v[APPEND ? kPage : 1][D + kVec];
 
   const int tid = threadIdx.x;
@@ -86,6 +109,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   }
   const int h0 = blockIdx.y * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, a.Hq + (APPEND ? 2 : 1) * a.Hkv);
 
+  if (tid < 4) s_y[256 * kVec + tid] = 0.f;
   // Cosines and sines, token by token.
   if (a.n_pairs && h0 < a.Hq + a.Hkv) {
     for (int e = tid; e < n_tok * a.n_pairs; e += 256) {
@@ -105,38 +129,27 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   // Rows at a time: nt tokens (a power of two) of kSlots / nt heads.
   int nt = 1;
   while (nt < n_tok && nt < kToks) nt *= 2;
-  float w[2][kVec];  // weights of this thread's values: queries, keys
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const void* p = i ? a.k_norm : a.q_norm;
-    if (!p) continue;
-#pragma unroll
-    for (int e = 0; e < kVec; ++e)
-      w[i][e] = a.norm_f32 || sizeof(T) == 4 ? static_cast<const float*>(p)[d0 + e]
-                                              : bf16_to_f32(static_cast<const uint16_t*>(p)[d0 + e]);
-  }
-
   const bool tile_v = n_tok > 1;  // values pass through LDS
-  const int h_rows = APPEND && !tile_v ? h1 : min(h1, a.Hq + a.Hkv);
   for (int t0 = 0; t0 < n_tok; t0 += nt) {
     const int t = t0 + slot % nt;
     const bool have = t < n_tok;
-    // element e turns with its partner: out = y c + partner sn
+    // Element e turns with its partner z: out = y c + z sn.  Where nothing turns z is a zero
+    // and sn minus zero, which leaves every y as it is.
     float c[kVec], sn[kVec];
-    int mate[kVec];  // partner's dimension, or -1
+    int mate[kVec / 4];  // half-split pairs: places in s_y of the partners of the four values from 4 i on
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const int d = d0 + e, n = a.n_pairs;
-      mate[e] = -1;
+      if (e % 4 == 0) mate[e / 4] = 256 * kVec;
       c[e] = 1.f;
-      sn[e] = 0.f;
+      sn[e] = -0.f;
       if (have && d < 2 * n) {
         const int i = a.interleaved ? d >> 1 : (d < n ? d : d - n);
         const bool second = a.interleaved ? (d & 1) : d >= n;
         const float2 x = s_cs[t][i];
         c[e] = x.x;
         sn[e] = second ? x.y : -x.y;
-        mate[e] = a.interleaved ? d ^ 1 : second ? d - n : d + n;
+        if (e % 4 == 0) mate[e / 4] = slot * D + (second ? d - n : d + n);
       }
     }
     int64_t qoff, koff, voff, qo, ko;
@@ -161,88 +174,118 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       if (a.n_str && (p < a.n_sink || p >= end - a.window))
         slot_at = p < a.n_sink ? p : a.n_sink + (p - a.n_sink) % a.window;
     }
-    for (int hb = h0; hb < h_rows; hb += kSlots / nt) {
-      const int h = hb + slot / nt;
-      const bool on = have && h < h_rows;
-      const int kind = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;  // query, key, value
-      const int g = kind == 0 ? h : kind == 1 ? h - a.Hq : h - a.Hq - a.Hkv;
-      u32x4 raw = {0u, 0u, 0u, 0u};
-      if (on) {
-        const T* src = kind == 0 ? static_cast<const T*>(a.q) + qoff + g * a.q_sh
-                                 : kind == 1 ? static_cast<const T*>(a.k) + koff + g * a.k_sh
-                                             : static_cast<const T*>(a.v) + voff + g * a.v_sh;
-        raw = ld16(src + d0);
+    // The heads of one kind (0: queries, 1: keys, 2: single tokens' values) in [lo, hi), the
+    // rows of the next two heads on their way while one is worked on.
+    auto heads = [&](auto kind_c, int lo, int hi, const T* src, int64_t sh, const void* norm, T* out, int64_t osh) {
+      constexpr int kind = decltype(kind_c)::value;
+      if (lo >= hi) return;
+      float w[kVec];
+      if (kind < 2 && norm) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          w[e] = a.norm_f32 || sizeof(T) == 4 ? static_cast<const float*>(norm)[d0 + e]
+                                              : bf16_to_f32(static_cast<const uint16_t*>(norm)[d0 + e]);
       }
-      const bool norm = kind == 0 ? a.q_norm != nullptr : kind == 1 && a.k_norm != nullptr;
-      if (a.n_pairs || a.q_norm || a.k_norm) {
-        float y[kVec];
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          if constexpr (sizeof(T) == 4) y[e] = __builtin_bit_cast(float, (uint32_t)raw[e]);
-          else y[e] = bf16_to_f32((uint16_t)(raw[e / 2] >> (16 * (e & 1))));
-        }
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) ss = fmaf(y[e], y[e], ss);
-#pragma unroll
-        for (int m = 1; m < kLanes; m *= 2) ss = wave_xor_sum(ss, m);
-        if (norm) {
-          const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) y[e] = y[e] * r * (kind ? w[1][e] : w[0][e]);
-        }
-        float z[kVec];
-        if (a.n_pairs) {
-          if (!a.interleaved) {  // partners in other lanes of the row
-#pragma unroll
-            for (int e = 0; e < kVec; e += 4) *reinterpret_cast<f32x4*>(&s_y[tid][e]) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
-            wave_lds_fence();
-            const float* line = &s_y[slot * kLanes][0];
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) z[e] = line[mate[e] < 0 ? 0 : mate[e]];
-            wave_lds_fence();
-          } else {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) z[e] = y[e ^ 1];
-          }
-#pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            if (mate[e] >= 0 && kind < 2) y[e] = fmaf(y[e], c[e], z[e] * sn[e]);
-        }
+      // whether head g's row goes anywhere
+      auto wanted = [&](int g) {
+        if (!have || g >= hi) return false;
+        return kind == 0 || !APPEND || (((a.streaming_mask >> g) & 1ull) ? slot_at : page) >= 0;
+      };
+      const int step = kSlots / nt;
+      int g = lo + slot / nt;
+      u32x4 raw = {0u, 0u, 0u, 0u}, next = raw;
+      const T* at_src = src + g * sh + d0;
+      const int64_t src_step = step * sh;
+      if (wanted(g)) raw = ld16(at_src);
+      if (wanted(g + step)) next = ld16(at_src + src_step);
+#pragma unroll 1
+      for (int hb = lo; hb < hi; hb += step, g += step) {
+        u32x4 later = {0u, 0u, 0u, 0u};
+        if (wanted(g + 2 * step)) later = ld16(at_src + 2 * src_step);
+        at_src += src_step;
         if (kind < 2 && (norm || a.n_pairs)) {
+          float y[kVec];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            if constexpr (sizeof(T) == 4) y[e] = __builtin_bit_cast(float, (uint32_t)raw[e]);
+            else y[e] = bf16_to_f32((uint16_t)(raw[e / 2] >> (16 * (e & 1))));
+          }
+          if (norm) {
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) ss = fmaf(y[e], y[e], ss);
+            const float r = 1.f / sqrtf(lanes_sum<kLanes>(ss) * (1.f / D) + a.eps);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) y[e] = y[e] * r * w[e];
+          }
+          if (a.n_pairs) {
+            float z[kVec];
+            if (a.interleaved) {
+#pragma unroll
+              for (int e = 0; e < kVec; ++e) z[e] = d0 + e < 2 * a.n_pairs ? y[e ^ 1] : 0.f;
+            } else {  // partners in other lanes of the row
+#pragma unroll
+              for (int e = 0; e < kVec; e += 4) *reinterpret_cast<f32x4*>(s_y + tid * kVec + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+              wave_lds_fence();
+              if (a.n_pairs % 4 == 0) {
+#pragma unroll
+                for (int e = 0; e < kVec; e += 4) {
+                  const f32x4 x = *reinterpret_cast<const f32x4*>(s_y + mate[e / 4]);
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) z[e + i] = x[i];
+                }
+              } else {
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) {
+                  const int d = d0 + e, n = a.n_pairs;
+                  z[e] = s_y[d < n ? slot * D + d + n : d < 2 * n ? slot * D + d - n : 256 * kVec];
+                }
+              }
+              wave_lds_fence();
+            }
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) y[e] = fmaf(y[e], c[e], z[e] * sn[e]);
+          }
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
             if constexpr (sizeof(T) == 4) raw[e] = __builtin_bit_cast(uint32_t, y[e]);
-            else if (e & 1) raw[e / 2] = (uint32_t)f32_to_bf16_bits(y[e - 1]) | ((uint32_t)f32_to_bf16_bits(y[e]) << 16);
+            else if (e & 1) raw[e / 2] = bf16_pair(y[e - 1], y[e]);
           }
         }
-      }
-      if (!on) continue;
-      if (kind == 0) {
-        st16(static_cast<T*>(a.q_out) + qo + g * a.qo_sh + d0, raw);
-      } else if (!APPEND) {
-        st16(static_cast<T*>(a.k_out) + ko + g * a.ko_sh + d0, raw);
-      } else {
-        const bool str = (a.streaming_mask >> g) & 1ull;
-        const int at = str ? slot_at : page;
-        if (at < 0) continue;
-        const int64_t unit = str ? ((int64_t)b * a.n_str + a.rank[g]) * a.ring_blocks + at / kPage : (int64_t)at * a.n_ret + a.rank[g];
-        const int r = (str ? at : p) % kPage;
-        if (kind == 1) {
-          st16(static_cast<T*>(str ? a.rk : a.pk) + unit * (kPage * D) + r * D + d0, raw);
-        } else {
-          T* dst = static_cast<T*>(str ? a.rv : a.pv) + unit * (kPage * D);
-          if (!str && a.v_token_major) {
-            st16(dst + r * D + d0, raw);
+        if (wanted(g)) {
+          if (kind == 0 || !APPEND) {
+            st16(out + g * osh + d0, raw);
           } else {
-            T x[kVec];
-            __builtin_memcpy(x, &raw, 16);
+            const bool str = (a.streaming_mask >> g) & 1ull;
+            const int at = str ? slot_at : page;
+            const int64_t unit = str ? ((int64_t)b * a.n_str + a.rank[g]) * a.ring_blocks + at / kPage : (int64_t)at * a.n_ret + a.rank[g];
+            const int r = (str ? at : p) % kPage;
+            if (kind == 1) {
+              st16(static_cast<T*>(str ? a.rk : a.pk) + unit * (kPage * D) + r * D + d0, raw);
+            } else {
+              T* dst = static_cast<T*>(str ? a.rv : a.pv) + unit * (kPage * D);
+              if (!str && a.v_token_major) {
+                st16(dst + r * D + d0, raw);
+              } else {
+                T x[kVec];
+                __builtin_memcpy(x, &raw, 16);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) dst[(d0 + e) * kPage + r] = x[e];
+                for (int e = 0; e < kVec; ++e) dst[(d0 + e) * kPage + r] = x[e];
+              }
+            }
           }
         }
+        raw = next;
+        next = later;
       }
-    }
+    };
+    heads(std::integral_constant<int, 0>{}, h0, min(h1, a.Hq), static_cast<const T*>(a.q) + qoff, a.q_sh, a.q_norm,
+          static_cast<T*>(a.q_out) + qo, a.qo_sh);
+    heads(std::integral_constant<int, 1>{}, max(0, h0 - a.Hq), min(h1 - a.Hq, a.Hkv), static_cast<const T*>(a.k) + koff, a.k_sh, a.k_norm,
+          static_cast<T*>(a.k_out) + ko, a.ko_sh);
+    if (APPEND && !tile_v)
+      heads(std::integral_constant<int, 2>{}, max(0, h0 - a.Hq - a.Hkv), h1 - a.Hq - a.Hkv, static_cast<const T*>(a.v) + voff, a.v_sh, nullptr,
+            static_cast<T*>(nullptr), 0);
   }
   if constexpr (APPEND) {
     if (!tile_v) return;
@@ -256,24 +299,46 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     }
     auto kept = [&](int p) { return p < a.n_sink || p >= end - a.window; };
     auto slot_of = [&](int p) { return p < a.n_sink ? p : a.n_sink + (p - a.n_sink) % a.window; };
-    for (int h = max(h0, a.Hq + a.Hkv); h < h1; ++h) {
+    const bool some = kept(p0) || kept(p0 + n_tok - 1);
+    // the first head from h on whose values go anywhere
+    auto next_head = [&](int h) {
+      while (h < h1 && !(((a.streaming_mask >> (h - a.Hq - a.Hkv)) & 1ull) ? some : page >= 0)) ++h;
+      return h;
+    };
+    constexpr int kPieces = (kPage * kLanes + 255) / 256;  // of a thread, a head
+    u32x4 piece[kPieces];
+    auto load = [&](int h) {
+      if (h >= h1) return;
+      const T* src = static_cast<const T*>(a.v) + b * a.v_sb + row0 * a.v_st + (h - a.Hq - a.Hkv) * a.v_sh;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int e = tid + 256 * i;
+        if (e < n_tok * kLanes) piece[i] = ld16(src + e / kLanes * a.v_st + e % kLanes * kVec);
+      }
+    };
+    int h = next_head(max(h0, a.Hq + a.Hkv));
+    load(h);
+    for (int ahead; h < h1; h = ahead) {
       const int g = h - a.Hq - a.Hkv;
       const bool str = (a.streaming_mask >> g) & 1ull;
-      if (str ? !(kept(p0) || kept(p0 + n_tok - 1)) : page < 0) continue;  // uniform
-      const T* src = static_cast<const T*>(a.v) + b * a.v_sb + row0 * a.v_st + g * a.v_sh;
+      ahead = next_head(h + 1);
       if (!str && a.v_token_major) {
         T* dst = static_cast<T*>(a.pv) + ((int64_t)page * a.n_ret + a.rank[g]) * (kPage * D);
-        for (int e = tid; e < n_tok * kLanes; e += 256) {
-          const int t = e / kLanes, d = e % kLanes * kVec;
-          st16(dst + (r0 + t) * D + d, ld16(src + t * a.v_st + d));
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int e = tid + 256 * i;
+          if (e < n_tok * kLanes) st16(dst + (r0 + e / kLanes) * D + e % kLanes * kVec, piece[i]);
         }
+        load(ahead);
         continue;
       }
       __syncthreads();  // the tile of the head before has been read
-      for (int e = tid; e < n_tok * kLanes; e += 256) {
-        const int t = e / kLanes, d = e % kLanes * kVec;
-        *reinterpret_cast<u32x4*>(&s_v[t][d]) = ld16(src + t * a.v_st + d);
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int e = tid + 256 * i;
+        if (e < n_tok * kLanes) *reinterpret_cast<u32x4*>(&s_v[e / kLanes][e % kLanes * kVec]) = piece[i];
       }
+      load(ahead);
       __syncthreads();
       // Whole 16-byte pieces where the tokens fill a page, or a block of the ring.
       bool whole = n_tok == kPage;
@@ -313,14 +378,18 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 }
 
 // Heads a workgroup: enough workgroups to fill the GPU first, then as many heads as
-// possible for each computation of the angles.
-constexpr int kRopeWgs = 1024;
+// possible for each computation of the angles.  Appends have sequences of different lengths
+// and fewer key and value heads that go anywhere, and take more and smaller workgroups: 16
+// packed prompts of 64 to 2900 tokens 137 us with 4096, 151 with 1024; a prompt of 8192 tokens without caches 38 us
+// with 1024, 52 with 4096.
+template <bool APPEND>
+constexpr int kRopeWgs = APPEND ? 4096 : 1024;
 
 template <int D, typename T, bool APPEND>
 static hipError_t launch(RopeArgs a, int64_t tiles, hipStream_t s) {
   const int heads = a.Hq + (APPEND ? 2 : 1) * a.Hkv;
   const int64_t all = tiles * (APPEND ? a.B : 1);
-  const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((kRopeWgs + all - 1) / all, (heads + 3) / 4));
+  const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((kRopeWgs<APPEND> + all - 1) / all, (heads + 3) / 4));
   a.heads_per_wg = (int)((heads + groups - 1) / groups);
   const int64_t gy = (heads + a.heads_per_wg - 1) / a.heads_per_wg;
   // The runtime takes a launch's work-items modulo 2^32, and a grid has at most 65535
