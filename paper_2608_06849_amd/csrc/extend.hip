@@ -39,6 +39,9 @@ __device__ __forceinline__ ExtendSeq extend_seq(const ExtendArgs& a, int b) {
   return s;
 }
 
+// Positions that a sequence's row of the block table has room for.
+__device__ __forceinline__ int paged_cap(const ExtendArgs& a) { return min(a.max_pages, kMaxPos / kPage) * kPage; }
+
 // Position that ring slot c holds when `start` tokens have been written, or -1.
 __device__ __forceinline__ int ring_position(int c, int start, int n_sink, int window) {
   if (c < n_sink) return c < start ? c : -1;
@@ -130,7 +133,7 @@ __device__ __forceinline__ SeqCost seq_cost(const ExtendArgs& a, const ExtendSeq
   SeqCost x;
   x.blocks = (int)(((int64_t)s.n * a.gs + ROWS - 1) / ROWS);
   const int n_new = div_up(s.n, TILE);
-  const int paged = div_up(min(s.start, a.max_pages * kPage), TILE);
+  const int paged = div_up(min(s.start, paged_cap(a)), TILE);
   const int ring = div_up(min(s.start, a.ring_cap), TILE);
   x.a[0] = (int64_t)kUnit * (a.item_cost + paged + min(n_new, a.block_tiles));
   x.c[0] = a.block_step;
@@ -188,7 +191,7 @@ __device__ __forceinline__ void set_visits(const ExtendArgs& a, ExtendItem& x) {
 }
 
 // Items go by head type, sequence, KV head and block of rows.  Every workgroup scans the
-// sequences (four a thread), each thread then writes items.
+// sequences (consecutive ones a thread), each thread then writes items.
 template <int ROWS, int TILE>
 __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
   __shared__ int64_t s_places[2][kPlanSeqs + 1];
@@ -197,18 +200,17 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
   __shared__ int64_t s_first[256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n_kv[2] = {a.n_ret, a.n_str};
-  int64_t x[3][4], sum[3] = {0, 0, 0};
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int b = 4 * tid + u;
-    ExtendSeq s = {0, 0, 0};
-    if (b < a.B) s = extend_seq(a, b);
-    const SeqCost k = seq_cost<ROWS, TILE>(a, s);
-    x[0][u] = n_kv[0] * places_of(k.a[0], k.c[0], k.blocks);
-    x[1][u] = n_kv[1] * places_of(k.a[1], k.c[1], k.blocks);
-    x[2][u] = k.blocks;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) sum[i] += x[i][u];
+  const int b0 = div_up(a.B, 256) * tid, b1 = min(b0 + div_up(a.B, 256), a.B);  // this thread's sequences
+  int64_t sum[3] = {0, 0, 0};
+#pragma unroll 1
+  for (int b = b0; b < b1; ++b) {
+    const SeqCost k = seq_cost<ROWS, TILE>(a, extend_seq(a, b));
+    for (int i = 0; i < 2; ++i) {
+      s_places[i][b] = n_kv[i] * places_of(k.a[i], k.c[i], k.blocks);
+      sum[i] += s_places[i][b];
+    }
+    s_blocks[b] = k.blocks;
+    sum[2] += k.blocks;
   }
   int64_t inc[3] = {sum[0], sum[1], sum[2]};
 #pragma unroll
@@ -222,20 +224,26 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) s_wave[i][wave] = inc[i];
   __syncthreads();
+  int64_t at[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    int64_t at = inc[i] - sum[i];
-    for (int w = 0; w < wave; ++w) at += s_wave[i][w];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (i < 2) s_places[i][4 * tid + u] = at;
-      else s_blocks[4 * tid + u] = (int)at;
-      at += x[i][u];
+    at[i] = inc[i] - sum[i];
+    for (int w = 0; w < wave; ++w) at[i] += s_wave[i][w];
+  }
+#pragma unroll 1
+  for (int b = b0; b < b1; ++b) {
+    for (int i = 0; i < 2; ++i) {
+      const int64_t own = s_places[i][b];
+      s_places[i][b] = at[i];
+      at[i] += own;
     }
-    if (tid == 255) {
-      if (i < 2) s_places[i][kPlanSeqs] = at;
-      else s_blocks[kPlanSeqs] = (int)at;
-    }
+    const int own = s_blocks[b];
+    s_blocks[b] = (int)at[2];
+    at[2] += own;
+  }
+  if (tid == 255) {
+    for (int i = 0; i < 2; ++i) s_places[i][kPlanSeqs] = at[i];
+    s_blocks[kPlanSeqs] = (int)at[2];
   }
   __syncthreads();
   const int blocks = s_blocks[kPlanSeqs];
@@ -243,17 +251,19 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
   const int64_t total = s_places[0][kPlanSeqs] + s_places[1][kPlanSeqs];
   const int64_t range = max(div64(total + a.wgs - 1, a.wgs), (int64_t)a.min_tiles * kUnit);
   const int used = (int)div64(total + range - 1, range);
-  if (blockIdx.x == 0 && tid == 0) {
-    *a.head = ExtendHead{total, range, used, n_items};
-    *a.copy = a;
+  if (blockIdx.x == 0 && tid == 0) *a.head = ExtendHead{total, range, used, n_items};
+  if (blockIdx.x == 0) {  // the arguments for a function that takes them from memory, word by word
+    static_assert(sizeof(ExtendArgs) % 4 == 0, "whole words");
+    const auto args = (const __attribute__((address_space(4))) uint32_t*)__builtin_amdgcn_kernarg_segment_ptr();
+    for (int i = tid; i < (int)(sizeof(ExtendArgs) / 4); i += 256) reinterpret_cast<uint32_t*>(a.copy)[i] = args[i];
   }
   const bool few = n_items <= 256;  // one item a thread of the first workgroup
   for (int idx = blockIdx.x * 256 + tid; idx < n_items; idx += gridDim.x * 256) {
     ExtendItem it;
     it.str = idx >= n_kv[0] * blocks;
     const int heads = n_kv[it.str], at = idx - (it.str ? n_kv[0] * blocks : 0);
-    int b = 0;  // the last sequence whose items begin at or before this one (and has some)
-    for (int hi = kPlanSeqs; hi - b > 1;) {
+    int b = 0;  // the last sequence whose items begin at or before this one
+    for (int hi = a.B; hi - b > 1;) {
       const int mid = (b + hi) >> 1;
       if ((int64_t)heads * s_blocks[mid] <= at) b = mid;
       else hi = mid;
@@ -277,7 +287,7 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
     it.ring = ((int64_t)b * a.n_str + it.rank) * a.ring_blocks;
     it.start = s.start;
     it.n_new = s.n;
-    it.cached = it.str ? min(s.start, a.ring_cap) : min(s.start, a.max_pages * kPage);
+    it.cached = it.str ? min(s.start, a.ring_cap) : min(s.start, paged_cap(a));
     it.row0 = rb * ROWS;
     it.t_first = div_gs(a, it.row0);
     it.t_last = div_gs(a, min(it.row0 + ROWS, s.n * a.gs) - 1);
@@ -350,7 +360,7 @@ __global__ __launch_bounds__(256) void extend_simple_kernel(ExtendArgs a) {
     const int64_t sb = a.cu_seqlens ? 0 : b;
     if (tid < D) s_q[tid] = value(a.q, sb * a.q_sb + (tok0 + t) * a.q_st + h * a.q_sh + tid);
     __syncthreads();
-    const int n_cached = str ? min(s.start, a.ring_cap) : min(s.start, a.max_pages * kPage);
+    const int n_cached = str ? min(s.start, a.ring_cap) : min(s.start, paged_cap(a));
     const int lo = a.evict ? s.start - a.window : s.start + t - a.window + 1;
     float m = -INFINITY, l = 0.f, o[kDims];
 #pragma unroll
@@ -1158,7 +1168,7 @@ static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
   if (a.out_f32) hipLaunchKernelGGL((extend_tile_kernel<D, ROWS, 3>), grid, dim3(2 * ROWS), 0, s, a);
   else hipLaunchKernelGGL((extend_tile_kernel<D, ROWS, 1>), grid, dim3(2 * ROWS), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL((extend_merge_kernel<D, ROWS>), dim3(a.wgs - 1, ROWS / 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((extend_merge_kernel<D, ROWS>), dim3(a.wgs - 1, (unsigned)((std::min<int64_t>(ROWS, (int64_t)a.T * a.gs) + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
