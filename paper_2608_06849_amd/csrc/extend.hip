@@ -945,16 +945,19 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       barrier();
 
+      auto next_kbs = [&](int it) __attribute__((always_inline)) {
+        const int kb_next = item.tile(it + 1 + Shape::kAhead) * kBN;
+#pragma unroll
+        for (int u = 0; u < Shape::kAhead; ++u) kbs[u] = kbs[u + 1];
+        kbs[Shape::kAhead] = kb_next;
+      };
       // Every wave runs MFMA, vector phase, MFMA, ..: waves 0-3 take the barrier of a tile
       // after its vector phase, waves 4-7 after its MFMA phase.
       auto vector_phase = [&](auto is_cached, int it) __attribute__((always_inline)) {
         if (grp == 1) sync_tile(it);
         valu_phase(is_cached, kbs[0]);
         if (grp == 0) sync_tile(it);
-        const int kb_next = item.tile(it + 1 + Shape::kAhead) * kBN;
-#pragma unroll
-        for (int u = 0; u < Shape::kAhead; ++u) kbs[u] = kbs[u + 1];
-        kbs[Shape::kAhead] = kb_next;
+        next_kbs(it);
       };
       auto run_tiles = [&](auto is_cached, int i0, int i1) __attribute__((always_inline)) {
         qk_part(at_k);
@@ -971,8 +974,16 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
         next_v(at_v);
       };
       const int mid = min(max(item.n_cached, v0), v1);
-      if (v0 < mid) run_tiles(kCached, v0, mid);
-      if (mid < v1) run_tiles(kNew, mid, v1);
+      if (item.row0 + wave * 32 < n_rows) {
+        if (v0 < mid) run_tiles(kCached, v0, mid);
+        if (mid < v1) run_tiles(kNew, mid, v1);
+      } else {  // a wave without rows takes part in the loads
+#pragma unroll 1
+        for (int it = v0; it < v1; ++it) {
+          sync_tile(it);
+          next_kbs(it);
+        }
+      }
 
       // Has a wave met what the loop above cannot take?  (The ring is free.)
       barrier();
