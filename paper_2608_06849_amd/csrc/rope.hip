@@ -16,9 +16,9 @@
 // The partners of a half-split pair meet in LDS within the wave.  Values of several tokens pass through an LDS tile into the
 // dimension-major V pages, single tokens are stored from the row.
 // Bound: memory, for single tokens the chain positions -> angles -> stores.  Measured: norms
-// and rotation of 8192 tokens (40 heads of 128, bf16) 39 us, 4.3 TB/s; 16 packed prompts
-// of 64 to 2900 tokens (48 heads) into caches 137 us, 3.8 TB/s (191 us with one row on its way and three
-// waves a SIMD); one token of 64 sequences 10 us.
+// and rotation of 8192 tokens (40 heads of 128, bf16) 52 us from HBM, 3.2 TB/s; 16 packed
+// prompts of 64 to 2900 tokens (48 heads) into caches 134 us, 3.9 TB/s (191 us with one row
+// on its way and three waves a SIMD); one token of 64 sequences 10 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -77,6 +77,7 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
   constexpr int kLanes = D / kVec;           // threads of a row
   constexpr int kSlots = 256 / kLanes;       // rows at a time
   constexpr int kToks = kSlots < kPage ? kSlots : kPage;
+  constexpr int kRowsAhead = 2;              // rows on their way: 3 cost registers, 16 packed prompts 139 us instead of 134
   __shared__ __align__(16) float2 s_cs[kPage][D / 2];
   __shared__ __align__(16) float s_y[256 * kVec + 4];  // and four zeros
   __shared__ __align__(16) T s_v[APPEND ? kPage : 1][D + kVec];
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
         slot_at = p < a.n_sink ? p : a.n_sink + (p - a.n_sink) % a.window;
     }
     // The heads of one kind (0: queries, 1: keys, 2: single tokens' values) in [lo, hi), the
-    // rows of the next two heads on their way while one is worked on.
+    // rows of the next kRowsAhead heads on their way while one is worked on.
     auto heads = [&](auto kind_c, int lo, int hi, const T* src, int64_t sh, const void* norm, T* out, int64_t osh) {
       constexpr int kind = decltype(kind_c)::value;
       if (lo >= hi) return;
@@ -193,15 +194,19 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
       };
       const int step = kSlots / nt;
       int g = lo + slot / nt;
-      u32x4 raw = {0u, 0u, 0u, 0u}, next = raw;
+      u32x4 raw = {0u, 0u, 0u, 0u}, ahead[kRowsAhead];
       const T* at_src = src + g * sh + d0;
       const int64_t src_step = step * sh;
       if (wanted(g)) raw = ld16(at_src);
-      if (wanted(g + step)) next = ld16(at_src + src_step);
+#pragma unroll
+      for (int u = 0; u + 1 < kRowsAhead; ++u) {
+        ahead[u] = u32x4{0u, 0u, 0u, 0u};
+        if (wanted(g + (u + 1) * step)) ahead[u] = ld16(at_src + (u + 1) * src_step);
+      }
 #pragma unroll 1
       for (int hb = lo; hb < hi; hb += step, g += step) {
-        u32x4 later = {0u, 0u, 0u, 0u};
-        if (wanted(g + 2 * step)) later = ld16(at_src + 2 * src_step);
+        ahead[kRowsAhead - 1] = u32x4{0u, 0u, 0u, 0u};
+        if (wanted(g + kRowsAhead * step)) ahead[kRowsAhead - 1] = ld16(at_src + kRowsAhead * src_step);
         at_src += src_step;
         if (kind < 2 && (norm || a.n_pairs)) {
           float y[kVec];
@@ -275,8 +280,9 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
             }
           }
         }
-        raw = next;
-        next = later;
+        raw = ahead[0];
+#pragma unroll
+        for (int u = 0; u + 1 < kRowsAhead; ++u) ahead[u] = ahead[u + 1];
       }
     };
     heads(std::integral_constant<int, 0>{}, h0, min(h1, a.Hq), static_cast<const T*>(a.q) + qoff, a.q_sh, a.q_norm,
@@ -380,8 +386,8 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
 // Heads a workgroup: enough workgroups to fill the GPU first, then as many heads as
 // possible for each computation of the angles.  Appends have sequences of different lengths
 // and fewer key and value heads that go anywhere, and take more and smaller workgroups: 16
-// packed prompts of 64 to 2900 tokens 137 us with 4096, 151 with 1024; a prompt of 8192 tokens without caches 38 us
-// with 1024, 52 with 4096.
+// packed prompts of 64 to 2900 tokens 134 us with 4096, 147 with 2048; a prompt of 8192 tokens without caches 52 us
+// with 1024, 70 with 4096, 57 with 512.
 template <bool APPEND>
 constexpr int kRopeWgs = APPEND ? 4096 : 1024;
 
