@@ -429,7 +429,9 @@ aoh_status aoh_extend(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_te
  * The same for packed tokens: q, out [total][Hq][D], k_new, v_new [total][Hkv][D];
  * sequence b's tokens are rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 (DEVICE int32
  * [batch + 1], ascending), at most max_new of them; a sequence may have none.
- * Rows behind the last sequence stay as they were.
+ * Rows behind the last sequence stay as they were.  With offsets that are not
+ * ascending, rows may get any sequence's results or none; nothing outside the
+ * tensors is touched.
  */
 aoh_status aoh_extend_varlen(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_tensor* v_new,
                              const int32_t* cu_seqlens, int32_t batch, int32_t max_new,

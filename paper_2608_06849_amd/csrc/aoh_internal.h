@@ -294,7 +294,7 @@ struct ExtendArgs {
   uint64_t gs_mul;              // ceil(2^36 / gs)
   // set by the launcher: workgroups, the fewest tiles of one; the partials of two blocks of
   // rows a workgroup, [2 wgs][rows][D] and (m in log2 units, l); the plan
-  int32_t wgs, min_tiles;
+  int32_t wgs, min_tiles, max_items;
   // cost of an item, in tiles; places from a block of rows to the next, new tiles that a block
   // spans, most tiles of a window and its sinks
   int32_t item_cost, block_step, block_tiles, band_tiles;

@@ -137,7 +137,7 @@ __device__ __forceinline__ SeqCost seq_cost(const ExtendArgs& a, const ExtendSeq
   const int ring = div_up(min(s.start, a.ring_cap), TILE);
   x.a[0] = (int64_t)kUnit * (a.item_cost + paged + min(n_new, a.block_tiles));
   x.c[0] = a.block_step;
-  // masked tiles of rings and windows take half as long again
+  // masked tiles of rings and windows take 2.5-3 us, those of a cached prefix 1.65
   x.a[1] = (int64_t)kUnit * a.item_cost + (kUnit * 3 / 2) * (int64_t)(a.evict ? ring + min(n_new, a.block_tiles) : min(ring + n_new, a.band_tiles));
   x.c[1] = a.evict ? a.block_step : 0;
   return x;
@@ -191,12 +191,14 @@ __device__ __forceinline__ void set_visits(const ExtendArgs& a, ExtendItem& x) {
 }
 
 // Items go by head type, sequence, KV head and block of rows.  Every workgroup scans the
-// sequences (consecutive ones a thread), each thread then writes items.
+// sequences (consecutive ones a thread), each thread then writes items.  Bound: the chain of
+// its loads and its own instructions' fetch, 5 us for one sequence, 7-8 for up to 24; in the
+// tile kernel itself the same work took more registers than its loops have left.
 template <int ROWS, int TILE>
 __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
   __shared__ int64_t s_places[2][kPlanSeqs + 1];
-  __shared__ int s_blocks[kPlanSeqs + 1];
-  __shared__ int64_t s_wave[3][4];
+  __shared__ int s_blocks[kPlanSeqs];
+  __shared__ int64_t s_wave[3][4], s_all;
   __shared__ int64_t s_first[256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n_kv[2] = {a.n_ret, a.n_str};
@@ -243,12 +245,13 @@ __global__ __launch_bounds__(256) void extend_plan_kernel(ExtendArgs a) {
   }
   if (tid == 255) {
     for (int i = 0; i < 2; ++i) s_places[i][kPlanSeqs] = at[i];
-    s_blocks[kPlanSeqs] = (int)at[2];
+    s_all = at[2];
   }
   __syncthreads();
-  const int blocks = s_blocks[kPlanSeqs];
+  // Sequences whose packed rows overlap may need more items than there is room for: none then.
+  const int blocks = (n_kv[0] + n_kv[1]) * s_all <= a.max_items ? (int)s_all : 0;
   const int n_items = (n_kv[0] + n_kv[1]) * blocks;
-  const int64_t total = s_places[0][kPlanSeqs] + s_places[1][kPlanSeqs];
+  const int64_t total = blocks ? s_places[0][kPlanSeqs] + s_places[1][kPlanSeqs] : 0;
   const int64_t range = max(div64(total + a.wgs - 1, a.wgs), (int64_t)a.min_tiles * kUnit);
   const int used = (int)div64(total + range - 1, range);
   if (blockIdx.x == 0 && tid == 0) *a.head = ExtendHead{total, range, used, n_items};
@@ -460,7 +463,11 @@ static hipError_t launch_simple(const ExtendArgs& a, hipStream_t s) {
 // bf16, many rows: a workgroup of ROWS rows, 32 a wave, on the 32x32x16 bf16 MFMA, with
 // 64-key tiles of K and V in LDS rings:
 //   S^T[64 keys x 32 rows] = K . Q^T,  softmax in fp32,  O^T[D x 32 rows] += V^T . P^T.
-// Bound: the matrix cores, and the LDS reads that feed them.
+// Bound: the matrix cores (busy 0.47 of the cycles), and the LDS reads and vector
+// instructions between them.  Measured (groups of 7, width 128): 4096 tokens after
+// 126976 3.96 ms, 1100 TFLOP/s; 2048 after 28672 450 us, 1004 TFLOP/s; chunks of four
+// sequences with eviction 195 us, 800 TFLOP/s.  Few rows: memory and the chain of one
+// wave, 4 tokens of 8 sequences at 32700 134 us, 3.9 TB/s.
 //  * Tiles move global -> LDS with direct loads, two or three tiles ahead.  K rows and new
 //    V rows are token-major with swizzled 16-byte chunks (PPTile); pages keep V
 //    dimension-major, [page][D][16 tokens], with the two halves of a dimension swapped in
@@ -1104,7 +1111,9 @@ __global__ __launch_bounds__(2 * ROWS, (D == 64 && PARTS == 1 ? 3 : 2)) void ext
 
 // ---------------------------------------------------------------------------
 // Items that several workgroups share: one row a wave, its lanes over groups of partials
-// and the dimensions.  The workgroups' x is the range that an item starts in.
+// and the dimensions.  The workgroups' x is the range that an item starts in.  Bound: the
+// partials' bytes (packed messages: 67 MB of 256-row blocks, 25-30 us), for few items the
+// chain head -> item -> partials, 8.5 us; eight rows one after the other in a wave took 60.
 template <int D, int ROWS>
 __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
   constexpr int kLanes = D / 4, kGroups = kWave / kLanes;
@@ -1158,8 +1167,13 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
 template <int D, int ROWS>
 static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
   a.wgs = a.cus * (ROWS == 256 ? 1 : D == 64 && !a.out_f32 ? 3 : 2);
+  // Smallest range: 17 tokens after 4093 36.6 us with 2 tiles, 43 with 1 (more partials to
+  // merge), 38.9 with 4.
   a.min_tiles = 2;
-  // an item's start costs as much as so many tiles (its first loads, its stores)
+  // An item's start costs as much as so many tiles (its first loads, its stores).  With 3, 8
+  // and 14 tiles blocks of 256 rows took 656, 588 and 518 us (2048 tokens after 28672) and 353,
+  // 286 and 296 (packed messages), blocks of 128 rows 155, 141 and 138 (4 tokens of 8
+  // sequences) and 34.7, 36.6 and 36.5 (17 tokens).
   a.item_cost = ROWS == 256 ? 12 : 8;
   a.block_step = std::max(1, kUnit * ROWS / (kBN * a.gs));
   a.block_tiles = ((ROWS + a.gs - 1) / a.gs + kBN - 1) / kBN;
@@ -1171,6 +1185,7 @@ static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
   a.items = reinterpret_cast<ExtendItem*>(a.copy + 1);
   const int64_t rows = (a.cu_seqlens ? std::min<int64_t>(a.total, (int64_t)a.B * a.T) : (int64_t)a.B * a.T) * a.gs;
   const int64_t n_items = (a.n_ret + a.n_str) * (rows / ROWS + a.B);  // at most
+  a.max_items = (int)n_items;
   a.first_item = reinterpret_cast<int32_t*>(a.items + n_items);
   const int plan_wgs = (int)std::min<int64_t>((n_items + 255) / 256, a.cus);
   hipLaunchKernelGGL((extend_plan_kernel<ROWS, kBN>), dim3(plan_wgs), dim3(256), 0, s, a);
@@ -1209,6 +1224,10 @@ hipError_t launch_extend(const ExtendArgs& a, int dtype, int d, hipStream_t s) {
       x.rv = static_cast<const uint16_t*>(a.rv) + ring;
     }
     hipError_t e;
+    // Blocks of 256 rows, one workgroup a CU, where a sequence can fill one: 2048 tokens after
+    // 28672 588 us (653 in blocks of 128), 4096 after 126976 4.30 ms (4.99); with two
+    // workgroups of 128 rows 4 tokens of 8 sequences take 135 us (153 in a block of 256),
+    // 17 tokens after 4093 28.6 (32).
     if (d == 64) e = launch_tiles<64, 128>(x, s);
     else if ((int64_t)a.T * a.gs >= 256) e = launch_tiles<128, 256>(x, s);
     else e = launch_tiles<128, 128>(x, s);

@@ -13,8 +13,9 @@
 // page) and a range of heads.  The tokens' cosines and sines are computed once into LDS;
 // a thread keeps one token and one 16-byte piece of its rows, so it reads its pairs'
 // values once and then goes over the heads, with the rows of the next two on their way.
-// The partners of a half-split pair meet in LDS within the wave.  Values of several tokens pass through an LDS tile into the
-// dimension-major V pages, single tokens are stored from the row.
+// The partners of a half-split pair meet in LDS within the wave.  Values of several tokens
+// pass through an LDS tile into the dimension-major V pages, single tokens are stored from
+// the row.
 // Bound: memory, for single tokens the chain positions -> angles -> stores.  Measured: norms
 // and rotation of 8192 tokens (40 heads of 128, bf16) 52 us from HBM, 3.2 TB/s; 16 packed
 // prompts of 64 to 2900 tokens (48 heads) into caches 134 us, 3.9 TB/s (191 us with one row
@@ -386,8 +387,8 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(RopeArgs a) {
 // Heads a workgroup: enough workgroups to fill the GPU first, then as many heads as
 // possible for each computation of the angles.  Appends have sequences of different lengths
 // and fewer key and value heads that go anywhere, and take more and smaller workgroups: 16
-// packed prompts of 64 to 2900 tokens 134 us with 4096, 147 with 2048; a prompt of 8192 tokens without caches 52 us
-// with 1024, 70 with 4096, 57 with 512.
+// packed prompts of 64 to 2900 tokens 134 us with 4096, 147 with 2048; a prompt of 8192
+// tokens without caches 52 us with 1024, 70 with 4096, 57 with 512.
 template <bool APPEND>
 constexpr int kRopeWgs = APPEND ? 4096 : 1024;
 

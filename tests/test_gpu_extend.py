@@ -17,8 +17,8 @@ import torch
 
 import synth
 from oracle import extend as oracle
-from paper_2608_06849_amd import (PagedCache, RingCache, aoh_extend, aoh_extend_varlen, aoh_kv_append, aoh_prefill,
-                                  aoh_prefill_chunked)
+from paper_2608_06849_amd import (PagedCache, RingCache, aoh_extend, aoh_extend_varlen, aoh_extend_workspace_bytes, aoh_kv_append,
+                                  aoh_prefill, aoh_prefill_chunked)
 from tests.helpers import bits, f64
 
 pytestmark = pytest.mark.gpu
@@ -353,3 +353,15 @@ def test_a_cache_beyond_four_gigabytes():
     run.check_counts(run.extend(F32))
     run.check_counts(run.extend(F32, append=True))
     assert np.array_equal(bits(k[pages - 7, :, 4:7].transpose(0, 1)), bits(run.k[0][100:103]))
+
+
+@pytest.mark.parametrize("d, out_dtype", [(128, BF), (64, F32)])
+def test_sequences_that_overlap_need_no_more_room_than_there_is(d, out_dtype):
+    """Offsets that are not ascending: 32 times all 600 rows, for which the workspace has no room."""
+    run = Run([0, 1], 4, d, 4, 28, [(0, 600)] + [(0, 0)] * 63)
+    q, k, v, _ = run.packed(0)
+    cu = i32([0, 600] * 32 + [600])
+    ws = torch.full((aoh_extend_workspace_bytes(64, 600, 8, 2, d) + 4096,), 5, dtype=torch.uint8, device=DEV)
+    out = torch.full(q.shape, 7.0, dtype=out_dtype, device=DEV)
+    aoh_extend_varlen(q, k, v, cu, 600, run.labels, None, run.full, run.ring, 4, 28, append=False, out=out, workspace=ws[:-4096])
+    assert (out == 7).all() and (ws[-4096:] == 5).all()
