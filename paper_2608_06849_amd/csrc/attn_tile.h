@@ -28,9 +28,11 @@ struct PPTile {
 // assembly so that the compiler does not treat every later LDS read as
 // possibly depending on it (it would wait for all outstanding loads before
 // each one); the kernel orders these loads itself with s_waitcnt and barriers.
+// Nor does it count hazards in there: a write of M0 needs one wait state before the
+// load, and the write comes right before it.
 __device__ __forceinline__ void lds_dma16(const void* gptr, const void* lds_row) {
   const uint32_t m0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds_row));
-  asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(gptr), "{m0}"(m0) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr), "{m0}"(m0) : "memory");
 }
 
 // s_waitcnt immediates (gfx9 encoding: vmcnt [3:0] and [15:14], expcnt [6:4],
