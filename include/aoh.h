@@ -412,7 +412,8 @@ aoh_status aoh_kv_append_rope_varlen(const aoh_tensor* q, const aoh_tensor* k_ne
  *     n_tokens new tokens in all, 16-byte aligned (fp32: none needed); a size for
  *     more sequences or tokens serves fewer.  Calls that share one must not overlap.
  * What a query does not see has no influence, whatever its bits: keys beyond it,
- * rows behind a sequence's end, slots and pages without a token.
+ * rows behind a sequence's end, slots and pages without a token.  An infinity in a V
+ * that it sees gives that infinity, however small its weight; both signs, or a NaN, NaN.
  * Dimension-major V pages only; Hq / Hkv <= 16; n_new <= 2^26, B n_new < 2^31.
  * Grids depend on shapes only (start_pos is read on the device), so calls can be
  * captured in HIP graphs.

@@ -325,6 +325,10 @@ __device__ __forceinline__ int range_of(int w, int used) {
   return (w >> 3) < per && r < used ? r : -1;
 }
 
+// x times a weight or a factor between weights: by the formula those are positive, so that an
+// infinity stays one where they fall below fp32's range.
+__device__ __forceinline__ float scaled(float x, float f) { return isinf(x) ? x : x * f; }
+
 // Four output values at element `at`.
 template <bool F32>
 __device__ __forceinline__ void store4(const ExtendArgs& a, int64_t at, f32x4 o) {
@@ -417,14 +421,14 @@ __global__ __launch_bounds__(256) void extend_simple_kernel(ExtendArgs a) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int i = 0; i < kDims; ++i) o[i] *= alpha;
+      for (int i = 0; i < kDims; ++i) o[i] = scaled(o[i], alpha);
       for (int i = 0; i < kWave; ++i) {
         const int64_t at = s_at[wave][i];
         if (at < 0) continue;
         const bool cached = k0 + i < n_cached;
         vp = cached ? (str ? a.rv : a.pv) : a.v;
 #pragma unroll
-        for (int u = 0; u < kDims; ++u) o[u] += s_p[wave][i] * value(vp, at + (int64_t)(lane + kWave * u) * (cached ? kPage : 1));
+        for (int u = 0; u < kDims; ++u) o[u] += scaled(value(vp, at + (int64_t)(lane + kWave * u) * (cached ? kPage : 1)), s_p[wave][i]);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -443,7 +447,7 @@ __global__ __launch_bounds__(256) void extend_simple_kernel(ExtendArgs a) {
         if (s_m[w] == -INFINITY && s_l[w] == 0.f) continue;  // no key (keys with NaN scores leave a NaN sum)
         const float f = s_m[w] == -INFINITY ? 1.f : expf(s_m[w] - M);
         L += f * s_l[w];
-        x += f * s_o[w][tid];
+        x += scaled(s_o[w][tid], f);
       }
       x /= L;
       const int64_t at = sb * a.o_sb + (tok0 + t) * a.o_st + h * a.o_sh + tid;
@@ -485,9 +489,11 @@ static hipError_t launch_simple(const ExtendArgs& a, hipStream_t s) {
 //    rounded, as in a prefill, for a third of the second product's time.
 // V behind a cache's last token is zeroed in LDS by the wave that loaded it.  Where a row
 // does not see a key that another row of the workgroup sees, V may be anything, and 0 V is
-// not 0 if it is not finite: the waves look for such values in the tiles that are masked,
-// and a workgroup that has met one (or a page outside the cache) takes its range again in
-// the careful loop.
+// not 0 if it is not finite: the waves look for such values in the tiles that are masked.
+// An infinity that a row does see times a part of its weight, or a weight, below the types'
+// range is NaN instead of infinite: the waves look for sums that are not finite.  A workgroup that
+// has met either (or a page outside the cache) takes its range again in the careful loop, which
+// sums the finite values and counts the others.
 template <int D, int ROWS>
 struct TileShape {
   static constexpr int kThreads = 2 * ROWS;
@@ -650,7 +656,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       new_k[jj] = 2u * ((uint32_t)r * (uint32_t)k_st + 8 * (pc ^ Tile::kx(r)));
       new_v[jj] = 2u * ((uint32_t)r * (uint32_t)v_st + 8 * (pc ^ Tile::vx(r)));
     }
-    bool bad = false;  // this wave has met a page outside the cache, or a V that the fast loop cannot take
+    bool bad = false;  // this wave has met a page outside the cache, or values that the fast loop cannot take
     auto issue_cached = [&](int slot_k, int slot_v, int entry_v) __attribute__((always_inline)) {
       int entry = uniform(entry_v);
       if (entry < 0 || entry >= end_page) {
@@ -872,7 +878,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
 #pragma unroll
         for (int mb = 0; mb < kMBlocks; ++mb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc_o[mb][i] *= alpha;
+          for (int i = 0; i < 16; ++i) acc_o[mb][i] = CAREFUL ? scaled(acc_o[mb][i], alpha) : acc_o[mb][i] * alpha;
         m_use = (m_run == -INFINITY) ? 0.f : m_run;
         tsum = exps();
       }
@@ -998,6 +1004,12 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
       if (item.row0 + wave * 32 < n_rows) {
         if (v0 < mid) run_tiles(kCached, v0, mid);
         if (mid < v1) run_tiles(kNew, mid, v1);
+        float zero = 0.f;  // NaN if a sum is not finite
+#pragma unroll
+        for (int mb = 0; mb < kMBlocks; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) zero = fmaf(acc_o[mb][i], 0.f, fmaf(acc_o[mb][i + 1], 0.f, zero));
+        bad = bad || __any(zero != zero);
       } else {  // a wave without rows takes part in the loads
 #pragma unroll 1
         for (int it = v0; it < v1; ++it) {
@@ -1046,7 +1058,9 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
 #pragma unroll
           for (int i = 0; i < 16; ++i) sacc[blk][i] = seen(place_of(blk, i)) ? sacc[blk][i] : -INFINITY;
         softmax_tile();
-        // P.V with the finite values, and NaN where a row sees one that is not
+        // P.V with the finite values; of the others that a row sees the infinities are counted in
+        // units of 1 and 128, NaNs in units of 16384 (a tile has 64 keys, so the counts are exact
+        // and keep apart).
 #pragma unroll
         for (int mb = 0; mb < kMBlocks; ++mb) {
           f32x16 hits;
@@ -1062,7 +1076,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
             for (int e = 0; e < 8; ++e) {
               const bool out = (bits[e] & 0x7f80) == 0x7f80;
               fin[e] = out ? (short)0 : bits[e];
-              ind[e] = (bf16)(out ? 1.f : 0.f);
+              ind[e] = (bf16)(!out ? 0.f : (bits[e] & 0x7f) ? 16384.f : bits[e] < 0 ? 128.f : 1.f);
               on[e] = (bf16)(seen(16 * ks + e) ? 1.f : 0.f);
             }
 #pragma unroll
@@ -1070,7 +1084,13 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
             hits = mfma32(ind, on, hits);
           }
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc_o[mb][i] = hits[i] > 0.f ? __builtin_nanf("") : acc_o[mb][i];
+          for (int i = 0; i < 16; ++i) {
+            const int n = (int)hits[i];
+            float x = acc_o[mb][i];
+            if (n & 0x7f) x += INFINITY;
+            if (n & 0x3f80) x -= INFINITY;
+            acc_o[mb][i] = n >> 14 ? __builtin_nanf("") : x;
+          }
         }
       }
     }
@@ -1149,25 +1169,33 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
   for (int w = rng + lane; w <= last; w += kWave) M = fmaxf(M, a.part_ml[slot(w) * 2]);
 #pragma unroll
   for (int i = 1; i < kWave; i *= 2) M = wave_xor_max(M, i);
-  float L = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int w = rng + lane / kLanes; w <= last; w += kGroups) {
-    const int64_t at = slot(w);
-    const float m = a.part_ml[at * 2], l = a.part_ml[at * 2 + 1];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + 4 * (lane % kLanes));
-    const bool none = m == -INFINITY && l == 0.f;
-    const float f = none ? 0.f : m == -INFINITY ? 1.f : fast_exp2(m - M);
-    L += f * l;
+  float L;
+  f32x4 o;
+  // INF: an infinity stays one where its factor is below fp32's range
+  auto join = [&](auto inf_c) __attribute__((always_inline)) {
+    constexpr bool INF = decltype(inf_c)::value;
+    L = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll(INF ? 1 : 8)
+    for (int w = rng + lane / kLanes; w <= last; w += kGroups) {
+      const int64_t at = slot(w);
+      const float m = a.part_ml[at * 2], l = a.part_ml[at * 2 + 1];
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + 4 * (lane % kLanes));
+      const bool none = m == -INFINITY && l == 0.f;
+      const float f = none ? 0.f : m == -INFINITY ? 1.f : fast_exp2(m - M);
+      L += f * l;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += none ? 0.f : f * x[e];
-  }
+      for (int e = 0; e < 4; ++e) o[e] += none ? 0.f : INF ? scaled(x[e], f) : f * x[e];
+    }
 #pragma unroll
-  for (int i = kLanes; i < kWave; i *= 2) {
-    L = wave_xor_sum(L, i);
+    for (int i = kLanes; i < kWave; i *= 2) {
+      L = wave_xor_sum(L, i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = wave_xor_sum(o[e], i);
-  }
+      for (int e = 0; e < 4; ++e) o[e] = wave_xor_sum(o[e], i);
+    }
+  };
+  join(std::integral_constant<bool, false>{});
+  if (__any(__builtin_isunordered(o[0], o[1]) || __builtin_isunordered(o[2], o[3]))) join(std::integral_constant<bool, true>{});
   if (lane >= kLanes) return;
   const float inv = 1.f / L;
 #pragma unroll
