@@ -414,6 +414,8 @@ aoh_status aoh_kv_append_rope_varlen(const aoh_tensor* q, const aoh_tensor* k_ne
  * What a query does not see has no influence, whatever its bits: keys beyond it,
  * rows behind a sequence's end, slots and pages without a token.  An infinity in a V
  * that it sees gives that infinity, however small its weight; both signs, or a NaN, NaN.
+ * A key whose score is -inf has weight 0 and no influence either; a row of nothing
+ * else is 0 / 0.
  * Dimension-major V pages only; Hq / Hkv <= 16; n_new <= 2^26, B n_new < 2^31.
  * Grids depend on shapes only (start_pos is read on the device), so calls can be
  * captured in HIP graphs.

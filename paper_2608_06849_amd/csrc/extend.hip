@@ -404,6 +404,7 @@ __global__ __launch_bounds__(256) void extend_simple_kernel(ExtendArgs a) {
         x = 0.f;
         for (int d = 0; d < D; ++d) x = fmaf(s_q[d], value(kp, ka + d), x);
         x *= a.scale;
+        if (x == -INFINITY) va = -1;  // weight 0
       }
       float mx = x;
 #pragma unroll
@@ -1077,7 +1078,7 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
               const bool out = (bits[e] & 0x7f80) == 0x7f80;
               fin[e] = out ? (short)0 : bits[e];
               ind[e] = (bf16)(!out ? 0.f : (bits[e] & 0x7f) ? 16384.f : bits[e] < 0 ? 128.f : 1.f);
-              on[e] = (bf16)(seen(16 * ks + e) ? 1.f : 0.f);
+              on[e] = (bf16)(sacc[ks >> 1][8 * (ks & 1) + e] == -INFINITY ? 0.f : 1.f);  // hidden, or weight 0
             }
 #pragma unroll
             for (int i = PARTS - 1; i >= 0; --i) acc_o[mb] = mfma32(__builtin_bit_cast(bf16x8, fin), pop[i][ks], acc_o[mb]);
