@@ -399,7 +399,8 @@ aoh_status aoh_kv_append_rope_varlen(const aoh_tensor* q, const aoh_tensor* k_ne
  *   out[b,t,h,:] = sum_j softmax_j(q[b,t,h,:] . k_j / sqrt(D)) v_j
  *   q: [B][n_new][Hq][D]; k_new, v_new: [B][n_new][Hkv][D]; out: [B][n_new][Hq][D],
  *     dtype of q, or fp32 for bf16 q (the weights then stay whole before the
- *     product with V, where a bf16 output takes them rounded to bf16).
+ *     product with V, where a bf16 output takes them rounded to bf16).  out
+ *     overlaps neither the inputs nor the caches.
  *   start_pos: DEVICE int32 [B] or NULL (0): the tokens that the caches hold.
  *     Positions beyond the block table and pages outside [0, num_pages) are not
  *     seen.  A sequence whose start_pos is negative or above 2^30 is left out:

@@ -850,7 +850,7 @@ def aoh_extend(q, k_new, v_new, head_is_streaming, start_pos, kv_full, kv_ring, 
     """Attention of new tokens q [B,n_new,Hq,D] at positions start_pos[b] + t (None: t) over the caches, which hold the
     positions before them, and over themselves (k_new, v_new [B,n_new,Hkv,D]); then, with append, K and V go into the
     caches.  evict: streaming heads see the cache as it was before the tokens (chunk eviction), else their per-token
-    window."""
+    window.  out must not overlap the inputs."""
     b, n = (q.shape[0], q.shape[1]) if q.dim() > 1 else (1, 1)
     return _extend("aoh_extend", q, k_new, v_new, (), b, b * n, head_is_streaming, start_pos, kv_full, kv_ring, n_sink, window,
                    evict, append, out, workspace, stream)

@@ -61,6 +61,12 @@ aoh_status extend_impl(const aoh_tensor* q, const aoh_tensor* k_new, const aoh_t
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(AOH_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
   }
 
+  // Rows are stored while others still read Q, K and V (of a range taken again, its own Q too).
+  const aoh_tensor* inputs[] = {q, k_new, v_new};
+  const char* names[] = {"q", "k_new", "v_new"};
+  for (int j = 0; j < 3; ++j)
+    if (out->data == inputs[j]->data) return fail(AOH_ERR_INVALID_ARG, "out in place of %s; it must overlap no input", names[j]);
+
   ExtendArgs a;
   std::memset(&a, 0, sizeof(a));
   const int i = nd - 3;  // the token axis
