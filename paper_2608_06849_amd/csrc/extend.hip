@@ -137,7 +137,9 @@ __device__ __forceinline__ SeqCost seq_cost(const ExtendArgs& a, const ExtendSeq
   const int ring = div_up(min(s.start, a.ring_cap), TILE);
   x.a[0] = (int64_t)kUnit * (a.item_cost + paged + min(n_new, a.block_tiles));
   x.c[0] = a.block_step;
-  // masked tiles of rings and windows take 2.5-3 us, those of a cached prefix 1.65
+  // Masked tiles of rings and windows take 2.5-3 us, those of a cached prefix 1.65.  (With
+  // eviction the ring's tiles are not masked.  Counted like the prefix's, chunks of four
+  // sequences took 196.5 us instead of 199.5, other calls the same within a run's noise of 1%.)
   x.a[1] = (int64_t)kUnit * a.item_cost + (kUnit * 3 / 2) * (int64_t)(a.evict ? ring + min(n_new, a.block_tiles) : min(ring + n_new, a.band_tiles));
   x.c[1] = a.evict ? a.block_step : 0;
   return x;
@@ -468,11 +470,14 @@ static hipError_t launch_simple(const ExtendArgs& a, hipStream_t s) {
 // bf16, many rows: a workgroup of ROWS rows, 32 a wave, on the 32x32x16 bf16 MFMA, with
 // 64-key tiles of K and V in LDS rings:
 //   S^T[64 keys x 32 rows] = K . Q^T,  softmax in fp32,  O^T[D x 32 rows] += V^T . P^T.
-// Bound: the matrix cores (busy 0.47 of the cycles), and the LDS reads and vector
-// instructions between them.  Measured (groups of 7, width 128): 4096 tokens after
-// 126976 3.96 ms, 1100 TFLOP/s; 2048 after 28672 450 us, 1004 TFLOP/s; chunks of four
-// sequences with eviction 195 us, 800 TFLOP/s.  Few rows: memory and the chain of one
-// wave, 4 tokens of 8 sequences at 32700 134 us, 3.9 TB/s.
+// Bound: no unit alone.  The matrix cores are busy 0.57 of the SIMDs' cycles in the longest
+// chunk measured and 0.50 in one of 2048 tokens, vector instructions (exponentials, masks,
+// conversions) 0.44 and 0.40, and they overlap in part.  Three parts of a weight at width 64:
+// vector instructions 0.53, matrix cores 0.31, with little overlap (no two waves of a block of
+// 128 rows run a phase apart).  Measured at width 128: 4096 tokens after 126976 (groups of 4)
+// 3.9-4.1 ms, 1060-1120 TFLOP/s; 2048 after 28672 (groups of 7) 440-470 us, about 1000 TFLOP/s;
+// chunks of four sequences with eviction (groups of 4) 192-204 us, about 790 TFLOP/s.  Few rows:
+// memory and the chain of one wave, 4 tokens of 8 sequences at 32700 (groups of 4) 134 us, 3.9 TB/s.
 //  * Tiles move global -> LDS with direct loads, two or three tiles ahead.  K rows and new
 //    V rows are token-major with swizzled 16-byte chunks (PPTile); pages keep V
 //    dimension-major, [page][D][16 tokens], with the two halves of a dimension swapped in
@@ -845,9 +850,12 @@ __device__ __forceinline__ bool extend_range(const ExtendArgs& a, TileRing<D, RO
           if constexpr (PARTS == 1 && ROWS == 128) {
             // The rounded weights' sum, so that they sum to 1 as the product takes them: a
             // fifth less error in the output (relative 0.0019 instead of 0.0023, its own
-            // rounding alone 0.0016).  Where the matrix cores are the bound the dot products
-            // cost 7% (4096 tokens after 126976 3.97 -> 4.39 ms), so blocks of 256 rows
-            // sum the weights as they were before the rounding.
+            // rounding alone 0.0016).  In blocks of 256 rows the dot products cost 7 to 12%
+            // (4096 tokens after 126976 3.99 -> 4.41 ms, 2048 after 28672 448 -> 480 us, packed
+            // messages 267 -> 298), so those sum the weights as they were before the rounding.
+            // In blocks of 128 they cost 1.3% at most, long chunks included (width 64: 2048 after
+            // 28672 344 -> 348 us, 4096 after 60000 1412 -> 1417, chunks with eviction 138 -> 133;
+            // width 128: 60 tokens of 8 sequences at 32700 211 -> 214).
             typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
             const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
             float s = 0.f;
@@ -1175,9 +1183,10 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
   // INF: an infinity stays one where its factor is below fp32's range
   auto join = [&](auto inf_c) __attribute__((always_inline)) {
     constexpr bool INF = decltype(inf_c)::value;
+    constexpr int kUnroll = INF ? 1 : 8;
     L = 0.f;
     o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll(INF ? 1 : 8)
+#pragma unroll kUnroll
     for (int w = rng + lane / kLanes; w <= last; w += kGroups) {
       const int64_t at = slot(w);
       const float m = a.part_ml[at * 2], l = a.part_ml[at * 2 + 1];
@@ -1210,13 +1219,15 @@ __global__ __launch_bounds__(256) void extend_merge_kernel(ExtendArgs a) {
 template <int D, int ROWS>
 static hipError_t launch_tiles(ExtendArgs a, hipStream_t s) {
   a.wgs = a.cus * (ROWS == 256 ? 1 : D == 64 && !a.out_f32 ? 3 : 2);
-  // Smallest range: 17 tokens after 4093 36.6 us with 2 tiles, 43 with 1 (more partials to
-  // merge), 38.9 with 4.
+  // Smallest range: 17 tokens after 4093 29.9 us with 2 tiles, 32.5 with 1 (more partials to
+  // merge), 34.9 with 4.
   a.min_tiles = 2;
-  // An item's start costs as much as so many tiles (its first loads, its stores).  With 3, 8
-  // and 14 tiles blocks of 256 rows took 656, 588 and 518 us (2048 tokens after 28672) and 353,
-  // 286 and 296 (packed messages), blocks of 128 rows 155, 141 and 138 (4 tokens of 8
-  // sequences) and 34.7, 36.6 and 36.5 (17 tokens).
+  // An item's start costs as much as so many tiles (its first loads, its stores).  No number is
+  // best for all calls, and these lie between.  Blocks of 256 rows with 8, 12, 14 and 20 tiles:
+  // 2048 tokens after 28672 486, 459, 457 and 455 us, packed messages 264, 271, 273 and 275, chunks
+  // of four sequences with eviction 194, 200, 202 and 209.  Blocks of 128 with 3, 8, 12 and 14:
+  // packed chunks of width 64 with fp32 outputs 612, 635, 650 and 658, with bf16 ones 396, 364, 357
+  // and 347, 4 tokens of 8 sequences at 32700 134 to 135 with each.
   a.item_cost = ROWS == 256 ? 12 : 8;
   a.block_step = std::max(1, kUnit * ROWS / (kBN * a.gs));
   a.block_tiles = ((ROWS + a.gs - 1) / a.gs + kBN - 1) / kBN;
@@ -1268,9 +1279,10 @@ hipError_t launch_extend(const ExtendArgs& a, int dtype, int d, hipStream_t s) {
     }
     hipError_t e;
     // Blocks of 256 rows, one workgroup a CU, where a sequence can fill one: 2048 tokens after
-    // 28672 588 us (653 in blocks of 128), 4096 after 126976 4.30 ms (4.99); with two
-    // workgroups of 128 rows 4 tokens of 8 sequences take 135 us (153 in a block of 256),
-    // 17 tokens after 4093 28.6 (32).
+    // 28672 448 us (534 in blocks of 128), 4096 after 126976 3.99 ms (4.48), 2048 after 28672
+    // packed with 32 single tokens at 4000 860 us (884); 200 tokens after 4000 packed with 63 single
+    // ones at 30000 721 (716).  Two workgroups of 128 rows a CU else: 4 tokens of 8 sequences at
+    // 32700 135 us (138 in blocks of 256), 17 tokens after 4093 29.9 (31.2).
     if (d == 64) e = launch_tiles<64, 128>(x, s);
     else if ((int64_t)a.T * a.gs >= 256) e = launch_tiles<128, 256>(x, s);
     else e = launch_tiles<128, 128>(x, s);

@@ -7,7 +7,8 @@
 //     (i, i + n) or (2 i, 2 i + 1), c and s = scale times cosine and sine of position
 //     times inv_freq[i]; values behind the first 2 n stay.
 // fp32 arithmetic, rounded once at the end.  The angle is reduced to a fraction of a turn
-// in fp64: its error stays below 2^-52 of the angle however far the position.
+// in fp64: its error stays below 2^-51 of the angle however far the position (three
+// roundings of half a step: position times frequency, the constant 1 / 2 pi, their product).
 //
 // A workgroup takes up to 16 tokens (appends: those of one 16-position block, so of one
 // page) and a range of heads.  The tokens' cosines and sines are computed once into LDS;
